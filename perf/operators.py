@@ -364,7 +364,7 @@ def _hold(s):
             case["rotary"], _BASE, layout=fs.FS_ROPE_HALVES if case["layout"] == "halves" else fs.FS_ROPE_PAIRS, scaling=kinds[case["scaling"]],
             factor=factor, low=low, high=high, original_positions=_ORIGINAL, amplitude=amplitude))
     if case["kind"] in ("decode", "step"):
-        s.batch = fs.make_batch(s.model, _LAYER, case["h"] * case["g"], s.scale, s.q, s.table, s.lens, s.out, s.lse,
+        s.batch = fs.make_batch(s.model, _LAYER, case["h"] * case["g"], s.scale, s.q if case["kind"] == "decode" else s.q_out, s.table, s.lens, s.out, s.lse,
                                 s.lens_host if case.get("lens_known") else None)
         s.ws = torch.empty(fs.fs_decode_workspace_bytes(s.pool, [s.batch]), dtype=torch.uint8, device="cuda")
     if case["kind"] == "prefill":
