@@ -34,7 +34,7 @@ extern "C" {
 typedef struct fs_pool fs_pool; /* opaque, owned by the library, released by fs_pool_destroy */
 typedef int32_t fs_model_t;     /* small index, valid until fs_model_unregister */
 
-enum fs_kv_dtype { FS_KV_FP16 = 0, FS_KV_FP8_E4M3 = 1, FS_KV_INT8 = 2, FS_KV_INT4 = 3 };
+enum fs_kv_dtype { FS_KV_FP16 = 0, FS_KV_FP8_E4M3 = 1, FS_KV_INT8 = 2, FS_KV_INT4 = 3, FS_KV_FP8_BLOCK = 4 };
 enum fs_src_dtype { FS_SRC_FP16 = 0, FS_SRC_FP32 = 1 };
 enum fs_status {
   FS_OK = 0,
@@ -50,7 +50,10 @@ enum fs_slab_state { FS_SLAB_FREE = 0, FS_SLAB_PARTIAL = 1, FS_SLAB_FULL = 2 };
  * chunk  K tile | V tile | K params | V params,  a tile row being one token's head_dim
  * elements (INT4: element 2j in the low nibble of byte j).  Params per token: INT8 one fp16
  * scale; INT4 fp16 scale then fp16 zero-point; FP16/FP8 none.  (Sec. 3.2 fixes only the two
- * size equations; this byte layout is the library's own.) */
+ * size equations; this byte layout is the library's own.)
+ * FP8_BLOCK: E4M3 codes, and behind a layer's head chunks (at n_kv_heads * head_chunk) two fp32 numbers for every KV
+ * head, the scales of its K and V rows in this block: powers of two, 2^-15 .. 2^7, so that every stored value (code x
+ * scale) is an fp16 number.  They need no table from the caller: see fs_kv_append. */
 typedef struct {
   int32_t kv_dtype, n_kv_heads, head_dim, n_layers;
   int32_t tokens_per_block, param_bytes;
@@ -148,6 +151,14 @@ int fs_model_dump_live(fs_pool* pool, fs_model_t model, uint8_t* live);
  *   block_tables : device int32 [n_seq][max_blocks]; entry [s][p / tokens_per_block] is the Blk ID
  * Quantizers (fp32, round-to-nearest-even, true division; finite inputs):
  *   FP16: nearest fp16.   FP8: nearest E4M3 of x / scale[layer][head], saturating at +-448.
+ *   FP8_BLOCK: nearest E4M3 of x / s, saturating at +-448, with one scale s = 2^e for the block's K (V) rows of a head:
+ *         the least e in -15 .. 7 with amax <= 448 * 2^e over the rows that the call brings the block, and never less
+ *         than the block's scale before the call -- a scale that grows takes the codes in front of the call's first slot
+ *         in the block and behind its last one along (nearest E4M3 of their value over the new scale).  A call that brings
+ *         a block's slot 0 begins the block anew: its earlier scale and whatever else it held are forgotten.  So a block is
+ *         filled from slot 0 on, call by call; within a call the tokens of one block must be neighbours in the list, without
+ *         a gap between their positions (as those of a prompt, a chunk or a decode step are), else that block's bytes are
+ *         undefined.
  *   INT8: s = fp16(amax/127) per (token, head) (1 if that is 0), q = clamp(rne(x/s), -127, 127).
  *   INT4: lo = min(x, 0), hi = max(x, 0) over the row, s = fp16((hi-lo)/15) (1 if 0),
  *         z = clamp(rne(-lo/s), 0, 15), q = clamp(rne(x/s) + z, 0, 15); z stored as fp16.
@@ -171,6 +182,79 @@ typedef struct {
   int64_t n_tokens;
 } fs_append_t;
 int fs_kv_append_multi(fs_pool* pool, const fs_append_t* appends, int n_appends, void* stream);
+
+/* ---- Rotary positions ---------------------------------------------------------------------------
+ * fs_model_set_rope gives a model its rotation: the first rotary_dim elements of a head's row are pairs, pair i =
+ * elements (i, i + rotary_dim / 2) (FS_ROPE_HALVES) or (2 i, 2 i + 1) (FS_ROPE_PAIRS); at position p pair (a, b) becomes
+ *   amplitude * (a cos(p f_i) - b sin(p f_i), b cos(p f_i) + a sin(p f_i)),
+ * the other elements stay as they are.  With g_i = base^(-2 i / rotary_dim), L = original_positions and turns(g) = L g / 2 pi:
+ *   FS_ROPE_UNSCALED:   f = g
+ *   FS_ROPE_LINEAR:     f = g / factor
+ *   FS_ROPE_BASE:       f = g with base * factor^(rotary_dim / (rotary_dim - 2)) for base (rotary_dim >= 4)
+ *   FS_ROPE_WAVELENGTH: f = g (1 - s) + (g / factor) s,  s = 1 - clamp((turns(g) - low) / (high - low), 0, 1): pairs that turn
+ *                       `high` times or more within the original positions keep their frequency, those that turn `low` times
+ *                       or less are stretched
+ *   FS_ROPE_DIMENSION:  the same with s linear in the pair's index, s = clamp((i - first) / max(last - first, 0.001), 0, 1),
+ *                       first = max(floor(at(high)), 0), last = min(ceil(at(low)), rotary_dim - 1),
+ *                       at(n) = rotary_dim ln(L / 2 pi n) / (2 ln base)
+ * Fields that a scaling does not name are not read.  rotary_dim: even, 2 .. head_dim; base > 1; factor, amplitude > 0;
+ * 0 <= low < high (DIMENSION: 0 < low).  Angles are exact to about 1e-9 turns at every position.  The call copies a table to
+ * the device synchronously, like fs_model_set_fp8_scales; calls that use the model must not be in flight.
+ * fs_rope_frequencies: the f_i, radians per position, to a host array of rotary_dim / 2.  Host only. */
+enum fs_rope_layout { FS_ROPE_HALVES = 0, FS_ROPE_PAIRS = 1 };
+enum fs_rope_scaling { FS_ROPE_UNSCALED = 0, FS_ROPE_LINEAR = 1, FS_ROPE_BASE = 2, FS_ROPE_WAVELENGTH = 3, FS_ROPE_DIMENSION = 4 };
+typedef struct {
+  int32_t rotary_dim, layout, scaling, original_positions;
+  double base, factor, low, high, amplitude;
+} fs_rope_t;
+int fs_model_set_rope(fs_pool* pool, fs_model_t model, const fs_rope_t* rope);
+int fs_rope_frequencies(const fs_rope_t* rope, double* radians);
+
+/* Rotates rows by themselves (queries of a model whose keys are cached rotated, rows to be rotated back):
+ *   x, out : device, [n_tokens] rows of n_heads x head_dim of src_dtype, 16-byte aligned; x_stride, out_stride: elements from
+ *            a token's rows to the next one's (0: n_heads * head_dim), multiples of 16 bytes.  out may be x (with its stride);
+ *            otherwise they must not overlap.
+ *   pos    : device int32 [n_tokens], the token's position; negative: padding, the token's rows of out are not written
+ *   inverse: non-zero = by the negative angles.  That is also the gradient's way back: with amplitude 1 the inverse rotation,
+ *            with any amplitude the transposed map.
+ * Computed in fp32, rounded once to src_dtype. */
+int fs_rope(fs_pool* pool, fs_model_t model, const void* x, int64_t x_stride, int n_heads, int src_dtype, const int32_t* pos,
+            int64_t n_tokens, int inverse, void* out, int64_t out_stride, void* stream);
+
+/* The new tokens of one layer between the projections and the attention call, in one launch: queries are rotated into q_out,
+ * keys are rotated and appended, values appended.  Same as fs_rope on the queries and fs_kv_append of the rotated fp32 keys (the
+ * keys are rounded once, to the cache's format).
+ *   q, k, v : device, [n_tokens] rows of n_q_heads (n_kv_heads) x head_dim of src_dtype; the strides are elements from a token's
+ *             rows to the next one's (0: the rows are contiguous), so that the three may be parts of one matrix.  16-byte aligned,
+ *             strides multiples of 16 bytes.  n_q_heads 0: keys and values alone, q and q_out are not read.
+ *   q_out   : device fp16 [n_tokens][n_q_heads][head_dim], what fs_decode_attention / fs_prefill_attention take; must not overlap
+ *             the sources
+ *   the other arguments as in fs_kv_append; pos is also what the rows are rotated by.  A token with a negative position is
+ *   padding: neither its q_out rows nor any cache bytes are written; one with a negative seq_idx, or whose table has no block of
+ *   the pool for it, has its queries rotated and nothing appended. */
+int fs_rope_append(fs_pool* pool, fs_model_t model, int layer, const void* q, int64_t q_stride, int n_q_heads, const void* k,
+                   int64_t k_stride, const void* v, int64_t v_stride, int src_dtype, const int32_t* seq_idx, const int32_t* pos,
+                   const int32_t* block_tables, int max_blocks, int64_t n_tokens, void* q_out, void* stream);
+
+/* ---- Block tables and token maps from the requests' lengths ----------------------------------------
+ * What a step's calls take per sequence and per token, built on the device in one launch, so that lengths that are only known
+ * there (tokens accepted by a verification, requests that ended) need no round trip to the host.  Request b holds held_lens[b]
+ * tokens (NULL: 0) and gets new_lens[b] more; with T = tokens_per_block it needs
+ *   ceil((held + new) / T) - ceil(held / T)
+ * further blocks, which it takes from block_ids (fs_blocks_alloc's, in the requests' order, on the device).  Written:
+ *   block_tables [n_seq][max_blocks]: entries ceil(held / T) .. of every row, -1 where block_ids ends before; no other entry
+ *   seq_lens [n_seq] = held + new;  q_offsets [n_seq + 1]: where the requests' new tokens begin, as fs_prefill_attention takes it
+ *   for i < n_tokens, the i-th new token in the requests' order:  seq_idx[i] and pos[i], as fs_kv_append takes them, and
+ *   slots[i] (or NULL) = Blk ID * T + slot in the block, the token's row in the pool; behind the last new token -1 in all three
+ *   (calls with a fixed number of tokens skip those), and -1 in slots where the token's block is none of the pool
+ *   status (or NULL): 0, or a bit mask -- 1: a length was negative or beyond max_blocks * T (clamped into 0 .. that); 2: block_ids or
+ *   the token lists were too short.  Tokens that find no place in the lists are cut: they count in neither seq_lens nor q_offsets.
+ * All device int32 (slots int64, status uint32); no two of the written arrays, and none of them and a read one, may overlap.
+ * block_tables' entries for the held tokens are read where slots is asked for. */
+int fs_batch_tables(fs_pool* pool, fs_model_t model, const int32_t* held_lens, const int32_t* new_lens, int n_seq,
+                    const int32_t* block_ids, int64_t n_block_ids, int32_t* block_tables, int max_blocks, int32_t* seq_lens,
+                    int32_t* q_offsets, int32_t* seq_idx, int32_t* pos, int64_t* slots, int64_t n_tokens, uint32_t* status,
+                    void* stream);
 
 /* ---- Decode attention (Sec. 2.1 / 2.3: one query per sequence reads all its cached tokens
  * through the block table as if the KV were contiguous) ---------------------------------------
@@ -337,7 +421,8 @@ enum fs_option {
   /* prefill kernel of the models with a head_dim of 128: 0 = automatic (default: the workgroup kernel, with items of 16
    * column blocks, or of 8 -- 8 or 4 behind long contexts -- where even those all find a compute unit of their own),
    * 1 / 2 / 4 = the wave-level kernels
-   * with 16 / 32 / 64 logit columns per wave, 16 = the workgroup kernel with items of 16 blocks */
+   * with 16 / 32 / 64 logit columns per wave, 16 = the workgroup kernel with items of 16 blocks.  (This option and the next
+   * two do not concern FP8_BLOCK models, whose kernel is the automatic one.) */
   FS_OPT_PREFILL_COLUMN_BLOCKS = 3,
   /* waves of the workgroup kernel at head_dim 128, launches with at least one item of 16 blocks per compute unit (or
    * FS_OPT_PREFILL_COLUMN_BLOCKS = 16): 0 or 8 = 8 x 32 columns (default), 4 = 4 x 64 columns */

@@ -13,7 +13,7 @@ import os
 import numpy as np
 import torch  # noqa: F401  -- first, so that libfineserve.so binds to the HIP runtime torch has already loaded
 
-FS_KV_FP16, FS_KV_FP8_E4M3, FS_KV_INT8, FS_KV_INT4 = 0, 1, 2, 3
+FS_KV_FP16, FS_KV_FP8_E4M3, FS_KV_INT8, FS_KV_INT4, FS_KV_FP8_BLOCK = 0, 1, 2, 3, 4
 FS_SRC_FP16, FS_SRC_FP32 = 0, 1
 FS_OK, FS_ERR_INVALID, FS_ERR_NOMEM, FS_ERR_STATE, FS_ERR_DEVICE = 0, -1, -2, -3, -4
 FS_SLAB_FREE, FS_SLAB_PARTIAL, FS_SLAB_FULL = 0, 1, 2
@@ -27,7 +27,7 @@ EXPORTS = ["fs_pool_create", "fs_pool_destroy", "fs_pool_base", "fs_model_regist
            "fs_model_set_fp8_scales", "fs_model_unregister", "fs_model_geometry", "fs_block_alloc", "fs_block_free",
            "fs_blocks_alloc", "fs_blocks_free",
            "fs_pool_stats", "fs_pool_dump", "fs_model_dump_live", "fs_kv_append", "fs_kv_append_multi", "fs_decode_step_multi",
-           "fs_decode_workspace_bytes",
+           "fs_decode_workspace_bytes", "fs_model_set_rope", "fs_rope_frequencies", "fs_rope", "fs_rope_append", "fs_batch_tables",
            "fs_decode_attention", "fs_decode_attention_multi", "fs_decode_attention_multi_static", "fs_decode_status", "fs_prefill_workspace_bytes",
            "fs_prefill_least_workspace_bytes", "fs_prefill_attention", "fs_sched_select_batch", "fs_sched_place_models", "fs_model_stats", "fs_pool_set_option",
            "fs_pool_get_option", "fs_pool_last_attention_kernel_ms", "fs_last_error"]
@@ -35,6 +35,10 @@ EXPORTS = ["fs_pool_create", "fs_pool_destroy", "fs_pool_base", "fs_model_regist
 (FS_OPT_DECODE_KERNEL, FS_OPT_SPLIT_BYTES, FS_OPT_KERNEL_TIMING, FS_OPT_PREFILL_COLUMN_BLOCKS, FS_OPT_PREFILL_WAVES,
  FS_OPT_PREFILL_PIPELINED, FS_OPT_PREFILL_STAGED_DEQUANT, FS_OPT_LAST_PREFILL_KERNEL, FS_OPT_DECODE_WORK_LIST,
  FS_OPT_LAST_DECODE_KERNEL, FS_OPT_LAST_PREFILL_ITEMS) = range(11)
+
+
+FS_ROPE_HALVES, FS_ROPE_PAIRS = 0, 1
+FS_ROPE_UNSCALED, FS_ROPE_LINEAR, FS_ROPE_BASE, FS_ROPE_WAVELENGTH, FS_ROPE_DIMENSION = range(5)
 
 
 class fs_geometry_t(ctypes.Structure):
@@ -55,6 +59,12 @@ class fs_model_stats_t(ctypes.Structure):
     _fields_ = [("slabs_partial", ctypes.c_int64), ("slabs_full", ctypes.c_int64), ("live_blocks", ctypes.c_int64),
                 ("free_blocks_in_partial_slabs", ctypes.c_int64), ("live_bytes", ctypes.c_uint64),
                 ("stranded_bytes", ctypes.c_uint64)]
+
+
+class fs_rope_t(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("original_positions", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("amplitude", ctypes.c_double)]
 
 
 class fs_append_t(ctypes.Structure):
@@ -99,6 +109,11 @@ def _load():
         "fs_model_dump_live": (i32, [vp, i32, vp]),
         "fs_kv_append": (i32, [vp, i32, i32, vp, vp, i32, vp, vp, vp, i32, i64, vp]),
         "fs_kv_append_multi": (i32, [vp, ctypes.POINTER(fs_append_t), i32, vp]),
+        "fs_model_set_rope": (i32, [vp, i32, ctypes.POINTER(fs_rope_t)]),
+        "fs_rope_frequencies": (i32, [ctypes.POINTER(fs_rope_t), vp]),
+        "fs_rope": (i32, [vp, i32, vp, i64, i32, i32, vp, i64, i32, vp, i64, vp]),
+        "fs_rope_append": (i32, [vp, i32, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp, vp, vp, i32, i64, vp, vp]),
+        "fs_batch_tables": (i32, [vp, i32, vp, vp, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp, vp]),
         "fs_decode_step_multi": (i32, [vp, ctypes.POINTER(fs_append_t), i32, ctypes.POINTER(fs_batch_t), i32, vp, u64, vp]),
         "fs_decode_workspace_bytes": (u64, [vp, ctypes.POINTER(fs_batch_t), i32]),
         "fs_decode_attention": (i32, [vp, i32, i32, i32, f32, vp, vp, vp, i32, i32, vp, vp, vp, u64, vp]),
@@ -331,6 +346,79 @@ def fs_kv_append(pool, model, layer, k_new, v_new, seq_idx, pos, block_tables, s
                              _dp(block_tables), block_tables.shape[1], seq_idx.numel(), _stream(stream))
     if rc != FS_OK:
         raise FsError(rc, "fs_kv_append")
+
+
+def make_rope(rotary_dim, base, layout=FS_ROPE_HALVES, scaling=FS_ROPE_UNSCALED, factor=1.0, low=0.0, high=0.0,
+              original_positions=0, amplitude=1.0) -> fs_rope_t:
+    return fs_rope_t(int(rotary_dim), layout, scaling, int(original_positions), float(base), float(factor), float(low), float(high),
+                     float(amplitude))
+
+
+def fs_model_set_rope(pool, model, rope: fs_rope_t):
+    rc = _L.fs_model_set_rope(pool, model, ctypes.byref(rope))
+    if rc != FS_OK:
+        raise FsError(rc, "fs_model_set_rope")
+
+
+def fs_rope_frequencies(rope: fs_rope_t) -> np.ndarray:
+    """Radians per position of every pair."""
+    out = np.empty(max(rope.rotary_dim // 2, 1), np.float64)
+    rc = _L.fs_rope_frequencies(ctypes.byref(rope), out.ctypes.data)
+    if rc != FS_OK:
+        raise FsError(rc, "fs_rope_frequencies")
+    return out
+
+
+def _token_stride(x):
+    """Elements from one token's [heads][head_dim] rows to the next one's; a token's rows themselves are contiguous."""
+    n, heads, d = x.shape
+    assert x.stride(2) == 1 and (heads <= 1 or x.stride(1) == d)
+    return x.stride(0) if n > 1 else 0
+
+
+def fs_rope(pool, model, x, pos, out, inverse=False, stream=None):
+    """x, out: CUDA fp16 or fp32 [n_tokens][n_heads][head_dim], a token's rows contiguous (out may be x); pos: CUDA int32 [n_tokens]."""
+    assert x.dtype == out.dtype and x.dtype in (torch.float16, torch.float32) and x.shape == out.shape
+    assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == x.shape[0]
+    rc = _L.fs_rope(pool, model, _dp(x), _token_stride(x), x.shape[1], FS_SRC_FP32 if x.dtype == torch.float32 else FS_SRC_FP16, _dp(pos),
+                    x.shape[0], int(inverse), _dp(out), _token_stride(out), _stream(stream))
+    if rc != FS_OK:
+        raise FsError(rc, "fs_rope")
+
+
+def fs_rope_append(pool, model, layer, q, k, v, seq_idx, pos, block_tables, q_out, stream=None):
+    """q: CUDA fp16 or fp32 [n_tokens][n_q_heads][head_dim] (None with q_out None: keys and values alone); k, v: [n_tokens][H][D] of the
+    same type, a token's rows contiguous; seq_idx, pos: CUDA int32 [n_tokens]; block_tables: CUDA int32 [n_seq][max_blocks]; q_out: fp16."""
+    assert k.dtype == v.dtype and k.dtype in (torch.float16, torch.float32) and k.shape == v.shape and block_tables.is_contiguous()
+    assert seq_idx.dtype == torch.int32 and pos.dtype == torch.int32 and block_tables.dtype == torch.int32
+    n = seq_idx.numel()
+    assert k.shape[0] == n == pos.numel() and seq_idx.is_contiguous() and pos.is_contiguous() and (q is None) == (q_out is None)
+    n_q = 0
+    if q is not None:
+        assert q.dtype == k.dtype and q.shape == q_out.shape and q.shape[0] == n and q_out.dtype == torch.float16 and q_out.is_contiguous()
+        n_q = q.shape[1]
+    rc = _L.fs_rope_append(pool, model, layer, _dp(q), _token_stride(q) if n_q else 0, n_q, _dp(k), _token_stride(k), _dp(v), _token_stride(v),
+                           FS_SRC_FP32 if k.dtype == torch.float32 else FS_SRC_FP16, _dp(seq_idx), _dp(pos), _dp(block_tables),
+                           block_tables.shape[1], n, _dp(q_out), _stream(stream))
+    if rc != FS_OK:
+        raise FsError(rc, "fs_rope_append")
+
+
+def fs_batch_tables(pool, model, held_lens, new_lens, block_ids, block_tables, seq_lens, q_offsets, seq_idx, pos, slots=None, status=None,
+                    stream=None):
+    """All CUDA int32 (slots int64, status one element of 32 bits or None): held_lens (or None), new_lens [n_seq]; block_ids [n]; written:
+    block_tables [n_seq][max_blocks], seq_lens [n_seq], q_offsets [n_seq + 1], seq_idx, pos, slots (or None) [n_tokens]."""
+    n_seq = new_lens.numel()
+    for t in (held_lens, new_lens, block_ids, block_tables, seq_lens, q_offsets, seq_idx, pos):
+        assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
+    assert block_tables.shape[0] == seq_lens.numel() == n_seq and q_offsets.numel() == n_seq + 1 and pos.numel() == seq_idx.numel()
+    assert held_lens is None or held_lens.numel() == n_seq
+    assert slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == pos.numel())
+    rc = _L.fs_batch_tables(pool, model, _dp(held_lens), _dp(new_lens), n_seq, _dp(block_ids), block_ids.numel(), _dp(block_tables),
+                            block_tables.shape[1], _dp(seq_lens), _dp(q_offsets), _dp(seq_idx), _dp(pos), _dp(slots), pos.numel(), _dp(status),
+                            _stream(stream))
+    if rc != FS_OK:
+        raise FsError(rc, "fs_batch_tables")
 
 
 def make_append(model, layer, k_new, v_new, seq_idx, pos, block_tables) -> fs_append_t:

@@ -4,7 +4,7 @@
 // the GPU, so one launch serves the newest tokens of all of them.
 #include <algorithm>
 
-#include "fs_append_rows.h"
+#include "fs_append_block.h"
 
 namespace fs {
 namespace {
@@ -20,9 +20,22 @@ __global__ __launch_bounds__(kWaves * 64) void kv_append_kernel(AppendArgs A) {
   append_rows<kSrcF32, DT, HP>(A, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves);
 }
 
-__global__ __launch_bounds__(kWaves * 64) void kv_append_multi_kernel(MultiAppendArgs P) { append_block(P, blockIdx.x, kWaves); }
+template <bool kSrcF32>
+__global__ __launch_bounds__(kWaves * 64) void kv_append_block_kernel(AppendArgs A) {
+  __shared__ float s_max[kWaves];
+  append_groups<kSrcF32, false, kWaves>(A, rope::RopeArgs{}, blockIdx.x, gridDim.x, s_max);
+}
+
+template <bool BLOCK>
+__global__ __launch_bounds__(kWaves * 64) void kv_append_multi_kernel(MultiAppendArgs P) { append_block<BLOCK>(P, blockIdx.x, kWaves); }
 
 }  // namespace
+
+int32_t group_chunk(int64_t n_tokens, int kinds, int64_t teams) {
+  int32_t c = 1;
+  while (c < 64 && n_tokens / (2 * c) * kinds >= teams) c *= 2;
+  return c;
+}
 
 int make_append_args(fs_pool* p, const fs_append_t& a, append::AppendArgs& A) {
   if (!p || a.model < 0 || a.model >= kMaxModels || !p->models[a.model].in_use) {
@@ -62,11 +75,14 @@ int make_append_args(fs_pool* p, const fs_append_t& a, append::AppendArgs& A) {
   int lpr_shift = 0;
   while ((append::kEpl << lpr_shift) < M.g.head_dim) ++lpr_shift;  // head_dim is a power of two >= 8
   A.lpr_shift = lpr_shift;
+  A.k_stride = A.v_stride = (int64_t)M.g.n_kv_heads * M.g.head_dim;
+  A.group_chunk = group_chunk(a.n_tokens, 2 * M.g.n_kv_heads, (int64_t)p->n_cu * 32);
   return FS_OK;
 }
 
 // Units of `hp` rows of an append (see append_rows).
 static int64_t append_units(const append::AppendArgs& A, int hp) {
+  if (A.g.dtype == FS_KV_FP8_BLOCK) return (A.n_tokens + A.group_chunk - 1) / A.group_chunk * 2 * A.g.H;
   const int64_t tpw = 64 >> A.lpr_shift;
   return (A.n_tokens + tpw - 1) / tpw * ((2 * (int64_t)A.g.H + hp - 1) / hp);
 }
@@ -84,7 +100,7 @@ uint32_t plan_append_blocks(const fs_pool* p, append::MultiAppendArgs& P, int wa
 
 hipError_t launch_append_multi(const fs_pool* p, append::MultiAppendArgs& P, hipStream_t s) {
   const uint32_t blocks = plan_append_blocks(p, P, kWaves);
-  hipLaunchKernelGGL(kv_append_multi_kernel, dim3(blocks), dim3(kWaves * 64), 0, s, P);
+  hipLaunchKernelGGL(P.any_block_scales() ? kv_append_multi_kernel<true> : kv_append_multi_kernel<false>, dim3(blocks), dim3(kWaves * 64), 0, s, P);
   return hipGetLastError();
 }
 
@@ -113,6 +129,16 @@ extern "C" int fs_kv_append(fs_pool* p, fs_model_t model, int layer, const void*
   if (p->n_cu == 0) {
     set_error("fs_kv_append: pool has no HIP device");
     return FS_ERR_DEVICE;
+  }
+  if (A.g.dtype == FS_KV_FP8_BLOCK) {  // a workgroup for every unit
+    A.group_chunk = group_chunk(n_tokens, 2 * A.g.H, (int64_t)p->n_cu * 8);
+    const int64_t teams = std::min<int64_t>(append_units(A, 1), (int64_t)p->n_cu * 64);
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(A.src_f32 ? kv_append_block_kernel<true> : kv_append_block_kernel<false>, dim3((unsigned)teams), dim3(kWaves * 64), 0,
+                       (hipStream_t)stream, A);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return device_error(e, "fs_kv_append launch");
+    return FS_OK;
   }
   const bool wide = append_units(A, kWideUnit) >= (int64_t)p->n_cu * 32;  // (32 wave slots of a compute unit)
   const int64_t blocks = std::min<int64_t>((append_units(A, wide ? kWideUnit : 1) + kWaves - 1) / kWaves, (int64_t)p->n_cu * 64);

@@ -40,7 +40,8 @@ struct AppendArgs {
   int64_t n_blocks;      // valid block ids are [0, n_blocks)
   int32_t layer, max_blocks;
   int32_t src_f32;       // source rows are fp32 (else fp16)
-  int32_t pad;
+  int32_t group_chunk;   // FP8_BLOCK: neighbouring tokens of a unit (see append_groups)
+  int64_t k_stride, v_stride;  // elements from one token's rows to the next's (append_rows: n_kv_heads * head_dim)
 };
 
 // Several appends in one launch: append i is worked on by the workgroups first_block[i] .. first_block[i + 1] - 1.
@@ -49,6 +50,11 @@ struct MultiAppendArgs {
   AppendArgs a[kMaxAppends];
   uint32_t first_block[kMaxAppends + 1];
   int32_t n;
+  bool any_block_scales() const {
+    for (int i = 0; i < n; ++i)
+      if (a[i].g.dtype == FS_KV_FP8_BLOCK) return true;
+    return false;
+  }
 };
 
 // max / min over the lanes of a row (lpr neighbouring lanes, lpr a power of two, the same in every lane): DPP within
@@ -325,35 +331,15 @@ __device__ __forceinline__ void append_rows(const AppendArgs& A, int64_t worker,
 // 84 / 79 / 73 / 82 us, FP16 -> INT8 103 / 87 / 82 / 89 us, fp32 -> INT4 124 / 120 / 122 / 123 us.
 constexpr int kWideUnit = 4;
 
-template <bool kSrcF32, int HP>
-__device__ __forceinline__ void append_any(const AppendArgs& A, int64_t worker, int64_t n_workers) {
-  switch (A.g.dtype) {
-    case FS_KV_FP16: append_rows<kSrcF32, FS_KV_FP16, HP>(A, worker, n_workers); break;
-    case FS_KV_FP8_E4M3: append_rows<kSrcF32, FS_KV_FP8_E4M3, HP>(A, worker, n_workers); break;
-    case FS_KV_INT8: append_rows<kSrcF32, FS_KV_INT8, HP>(A, worker, n_workers); break;
-    default: append_rows<kSrcF32, FS_KV_INT4, HP>(A, worker, n_workers); break;
-  }
-}
-
-// The workgroup's share of a multi-append launch: `block` = its index among the launch's append workgroups,
-// `waves` = waves per workgroup.
-__device__ __forceinline__ void append_block(const MultiAppendArgs& P, uint32_t block, int waves) {
-  int i = 0;
-  while (i + 1 < P.n && block >= P.first_block[i + 1]) ++i;
-  const AppendArgs& A = P.a[i];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t worker = (int64_t)(block - P.first_block[i]) * waves + wave;
-  const int64_t n_workers = (int64_t)(P.first_block[i + 1] - P.first_block[i]) * waves;
-  if (A.src_f32) append_any<true, 1>(A, worker, n_workers);
-  else append_any<false, 1>(A, worker, n_workers);
-}
-
 }  // namespace append
 
 // Host side (fs_append.hip): validates one append and fills its kernel arguments; sizes a multi-append launch for
 // workgroups of `waves` waves (first_block, n; returns the number of workgroups).
 int make_append_args(fs_pool* p, const fs_append_t& a, append::AppendArgs& out);
 uint32_t plan_append_blocks(const fs_pool* p, append::MultiAppendArgs& P, int waves);
+// FP8_BLOCK: neighbouring tokens that a unit looks for groups in, a power of two up to 64: one where the launch has few tokens, each
+// perhaps a group of its own (a decode step), more while `teams` have a unit each (a prompt's groups are whole blocks).
+int32_t group_chunk(int64_t n_tokens, int kinds, int64_t teams);
 hipError_t launch_append_multi(const fs_pool* p, append::MultiAppendArgs& P, hipStream_t s);
 
 }  // namespace fs

@@ -197,7 +197,13 @@ struct ItemCtx {
   int T, R;
   uint32_t r_magic;           // ceil(2^32 / R)
   uint64_t base_off = 0;      // added to every address of the table
+  uint64_t scale_off = 0;     // FP8_BLOCK: from a head chunk to the head's scales in the block (scale_offset)
 };
+
+// FP8_BLOCK: the scales lie behind a layer's head chunks (see fs_geometry_t).
+__device__ __host__ inline uint64_t scale_offset(const DevGeom& g, int head) {
+  return (uint64_t)(g.H - head) * g.head_chunk + 8u * (uint32_t)head;
+}
 
 // run / R  (r_magic = ceil(2^32 / R) does not fit 32 bits for R = 1; exact while run * R < 2^32)
 __device__ __host__ inline int div_runs(int vr, int R, uint32_t r_magic) {

@@ -12,7 +12,7 @@
 #include <cstdlib>
 #include <vector>
 
-#include "fs_append_rows.h"
+#include "fs_append_block.h"
 #include "fs_attention.h"
 
 // Workspace of fs_decode_attention_multi_static, the entry point for callers that cannot allocate: one copy per
@@ -173,9 +173,10 @@ __global__ __launch_bounds__(kPrepThreads) void prep_kernel(MultiArgs A) { prep_
 
 // Front kernel of a decode step: the first kPrepGroups workgroups prepare the work list, the others append the
 // step's new K/V rows.  Neither reads what the other writes, so they share one launch.
+template <bool BLOCK>
 __global__ __launch_bounds__(kPrepThreads) void step_front_kernel(MultiArgs A, append::MultiAppendArgs P) {
   if (blockIdx.x < kPrepGroups) prep_body(A, blockIdx.x, kPrepGroups);
-  else append::append_block(P, blockIdx.x - kPrepGroups, kPrepThreads / 64);
+  else append::append_block<BLOCK>(P, blockIdx.x - kPrepGroups, kPrepThreads / 64);
 }
 static_assert(sizeof(MultiArgs) + sizeof(append::MultiAppendArgs) <= 4096, "kernel arguments of the front kernel");
 
@@ -361,7 +362,7 @@ hipError_t launch_prep(const MultiArgs& A, hipStream_t s) {
 
 hipError_t launch_step_front(const fs_pool* p, const MultiArgs& A, append::MultiAppendArgs& P, hipStream_t s) {
   const uint32_t append_blocks = plan_append_blocks(p, P, kPrepThreads / 64);
-  hipLaunchKernelGGL(step_front_kernel, dim3(kPrepGroups + append_blocks), dim3(kPrepThreads), 0, s, A, P);
+  hipLaunchKernelGGL(P.any_block_scales() ? step_front_kernel<true> : step_front_kernel<false>, dim3(kPrepGroups + append_blocks), dim3(kPrepThreads), 0, s, A, P);
   return hipGetLastError();
 }
 
@@ -569,6 +570,7 @@ struct DirectRate {
 DirectRate direct_rate(const fs_geometry_t& g) {
   switch (g.kv_dtype) {
     case FS_KV_FP16: return g.head_dim == 256 ? DirectRate{33, 6200} : DirectRate{49, 6500};
+    case FS_KV_FP8_BLOCK:  // (the same rows, two scales a block beside them)
     case FS_KV_FP8_E4M3: return g.head_dim == 64 ? DirectRate{33, 5600} : DirectRate{44, 6500};
     case FS_KV_INT8: return g.head_dim == 64 ? DirectRate{29, 5400} : DirectRate{38, 6500};
     default: {
@@ -657,7 +659,7 @@ bool plan_direct(const fs_pool* p, const fs_batch_t* batches, int n_batches, con
     sum_us += (double)sum / rate[i].wg;
     all_us += (double)sum / rate[i].chip;
     int4_only = int4_only && g.kv_dtype == FS_KV_INT4;
-    memory_bound = memory_bound || g.kv_dtype == FS_KV_FP16 || (g.kv_dtype == FS_KV_FP8_E4M3 && g.head_dim > 64);
+    memory_bound = memory_bound || g.kv_dtype == FS_KV_FP16 || ((g.kv_dtype == FS_KV_FP8_E4M3 || g.kv_dtype == FS_KV_FP8_BLOCK) && g.head_dim > 64);
   }
   // one workgroup checks all entries, about 3500 per us
   if ((double)entries / 3500 > 1.2 * all_us + 10) return false;

@@ -52,6 +52,11 @@ __device__ __forceinline__ void load8<FS_KV_FP8_E4M3>(const uint8_t* p, float (&
 }
 
 template <>
+__device__ __forceinline__ void load8<FS_KV_FP8_BLOCK>(const uint8_t* p, float (&x)[8]) {
+  load8<FS_KV_FP8_E4M3>(p, x);
+}
+
+template <>
 __device__ __forceinline__ void load8<FS_KV_INT8>(const uint8_t* p, float (&x)[8]) {
   const uint2 v = *reinterpret_cast<const uint2*>(p);
 #pragma unroll
@@ -137,7 +142,11 @@ __device__ void process_item(const MultiArgs& A, int b, int seq, int chunk, int 
       load8<DT>(chunkp + (uint64_t)tib * g.row_bytes + lig * kElemBytes8, kf);
       load8<DT>(chunkp + g.kv_tile + (uint64_t)tib * g.row_bytes + lig * kElemBytes8, vf);
       float ks = k_static, vs = v_static;
-      if (DT == FS_KV_INT8) {
+      if (DT == FS_KV_FP8_BLOCK) {
+        const float* sc = reinterpret_cast<const float*>(chunkp + scale_offset(g, head));
+        ks = sc[0];
+        vs = sc[1];
+      } else if (DT == FS_KV_INT8) {
         const uint8_t* par = chunkp + 2u * g.kv_tile;
         ks = half_bits_to_f32(*reinterpret_cast<const uint16_t*>(par + 2 * tib));
         vs = half_bits_to_f32(*reinterpret_cast<const uint16_t*>(par + g.par_tile + 2 * tib));
@@ -231,6 +240,7 @@ __device__ __forceinline__ void dispatch_dtype(const MultiArgs& A, int b, int se
     case FS_KV_FP16: dispatch_gp<FS_KV_FP16>(A, b, seq, chunk, head, item, smem, qrow, len_override); break;
     case FS_KV_FP8_E4M3: dispatch_gp<FS_KV_FP8_E4M3>(A, b, seq, chunk, head, item, smem, qrow, len_override); break;
     case FS_KV_INT8: dispatch_gp<FS_KV_INT8>(A, b, seq, chunk, head, item, smem, qrow, len_override); break;
+    case FS_KV_FP8_BLOCK: dispatch_gp<FS_KV_FP8_BLOCK>(A, b, seq, chunk, head, item, smem, qrow, len_override); break;
     default: dispatch_gp<FS_KV_INT4>(A, b, seq, chunk, head, item, smem, qrow, len_override); break;
   }
 }

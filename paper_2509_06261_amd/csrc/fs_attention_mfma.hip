@@ -93,6 +93,7 @@ __device__ __forceinline__ void stream_item(const MultiArgs& A, const ItemPlan& 
   X.v_end = P.v1;
   X.k0 = P.k0;
   X.chunk_ptr = s_ptr;
+  if constexpr (DT == FS_KV_FP8_BLOCK) X.scale_off = scale_offset(g, head);
 
   // Q operand and per-head constants
   u32x4 qb[HD / 32];
@@ -236,7 +237,8 @@ __device__ __forceinline__ void leave_records(const MultiArgs& A, const ItemPlan
 }
 
 // step 0: stream_item, step 1: finish_item, step 2: stream_item and leave_records
-template <int STEP, int GP, int HD>
+// BLOCK: a kernel of its own for launches with FP8_BLOCK batches, so that the others' kernels stay as small as they are.
+template <int STEP, int GP, int HD, bool BLOCK>
 __device__ __forceinline__ void dispatch_dtype(const MultiArgs& A, const ItemPlan& P, uint64_t* s_ptr, StateT<HD>& st,
                                                const uint64_t* part_off, float* rec) {
   switch (A.b[P.b].g.dtype) {
@@ -252,21 +254,26 @@ __device__ __forceinline__ void dispatch_dtype(const MultiArgs& A, const ItemPla
     case FS_KV_FP16: FS_STEP(FS_KV_FP16);
     case FS_KV_FP8_E4M3: FS_STEP(FS_KV_FP8_E4M3);
     case FS_KV_INT8: FS_STEP(FS_KV_INT8);
+    case FS_KV_FP8_BLOCK:
+      if constexpr (BLOCK) {
+        FS_STEP(FS_KV_FP8_BLOCK);
+      }
+      [[fallthrough]];
     default: FS_STEP(FS_KV_INT4);
 #undef FS_STEP
   }
 }
 
-template <int STEP, int HD>
+template <int STEP, int HD, bool BLOCK>
 __device__ __forceinline__ void dispatch_item(const MultiArgs& A, const ItemPlan& P, uint64_t* s_ptr, StateT<HD>& st,
                                               const uint64_t* part_off, float* rec = nullptr) {
-  if (A.b[P.b].G <= 4) dispatch_dtype<STEP, 4, HD>(A, P, s_ptr, st, part_off, rec);
-  else dispatch_dtype<STEP, 16, HD>(A, P, s_ptr, st, part_off, rec);
+  if (A.b[P.b].G <= 4) dispatch_dtype<STEP, 4, HD, BLOCK>(A, P, s_ptr, st, part_off, rec);
+  else dispatch_dtype<STEP, 16, HD, BLOCK>(A, P, s_ptr, st, part_off, rec);
 }
 
-// One kernel per head_dim (every batch of a launch has the same one).
-template <int HD>
-__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_attention_kernel(MultiArgs A, int table_entries) {
+// One kernel per head_dim (every batch of a launch has the same one), and one for launches with FP8_BLOCK batches.
+template <int HD, bool BLOCK>
+__device__ __forceinline__ void attention_grid(const MultiArgs& A, int table_entries) {
   extern __shared__ uint64_t smem64[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -350,11 +357,11 @@ __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_attention_
     ++tl_items;
 #endif
     StateT<HD> st;
-    dispatch_item<0, HD>(A, P, s_ptr, st, s_part_off);
+    dispatch_item<0, HD, BLOCK>(A, P, s_ptr, st, s_part_off);
 #ifdef FS_TIMELINE
     const uint64_t tl_tiles = wall_clock64();
 #endif
-    dispatch_item<1, HD>(A, P, s_ptr, st, s_part_off);
+    dispatch_item<1, HD, BLOCK>(A, P, s_ptr, st, s_part_off);
 #ifdef FS_TIMELINE
     if (lane == 0 && item < kTimelineItems) {
       uint64_t* row = A.timeline + 8 * (kTimelineWaves + item);
@@ -376,6 +383,15 @@ __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_attention_
     row[3] = __builtin_amdgcn_s_getreg(20 | (0 << 6) | (3 << 11)) & 7;  // hwreg(HW_REG_XCC_ID, 0, 4)
   }
 #endif
+}
+
+template <int HD>
+__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_attention_kernel(MultiArgs A, int table_entries) {
+  attention_grid<HD, false>(A, table_entries);
+}
+template <int HD>
+__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_block_attention_kernel(MultiArgs A, int table_entries) {
+  attention_grid<HD, true>(A, table_entries);
 }
 
 // ---- Direct launches: one workgroup per (sequence, split, KV head), no work list ------------------------------------
@@ -488,8 +504,8 @@ __device__ __forceinline__ void merge_records(const MultiArgs& A, const ItemPlan
   }
 }
 
-template <int HD>
-__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_direct_kernel(DirectArgs D, uint32_t* status) {
+template <int HD, bool BLOCK>
+__device__ __forceinline__ void direct_item_of_grid(const DirectArgs& D, uint32_t* status) {
   extern __shared__ uint64_t s_tab[];
   __shared__ float2 s_before[2][16];
   if (blockIdx.x == 0) {
@@ -551,7 +567,7 @@ __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_direct_ker
     __syncthreads();
     if (P.v0 < P.v1) {  // wave-uniform
       StateT<HD> unused;
-      dispatch_item<2, HD>(A, P, s_tab, unused, nullptr, rec);
+      dispatch_item<2, HD, BLOCK>(A, P, s_tab, unused, nullptr, rec);
     } else if (lane < G) {
       *reinterpret_cast<float2*>(rec + lane * (HD + 2) + HD) = float2{-INFINITY, 0.f};
     }
@@ -570,6 +586,15 @@ __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_direct_ker
   }
 }
 
+template <int HD>
+__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_direct_kernel(DirectArgs D, uint32_t* status) {
+  direct_item_of_grid<HD, false>(D, status);
+}
+template <int HD>
+__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_block_direct_kernel(DirectArgs D, uint32_t* status) {
+  direct_item_of_grid<HD, true>(D, status);
+}
+
 }  // namespace
 
 // Shapes this kernel covers: head_dim 64, 128 or 256, at least 8 tokens per block (a run of 8 slots fits a block),
@@ -581,16 +606,25 @@ bool mfma_supports(const DevBatch& b) {
   return max_tok < (1ull << 31) && max_run * (uint64_t)b.R < (1ull << 32);
 }
 
+static bool any_block_scales(const MultiArgs& A) {
+  for (int i = 0; i < A.n_batches; ++i)
+    if (A.b[i].g.dtype == FS_KV_FP8_BLOCK) return true;
+  return false;
+}
+
 hipError_t launch_mfma(const MultiArgs& A, int n_workgroups, hipStream_t s) {
   // LDS: per wave one 8-byte address per block of the largest split (+ slack)
   int entries = 0;
   for (int i = 0; i < A.n_batches; ++i) entries = std::max(entries, A.b[i].chunk_runs / A.b[i].R + 4);
   const size_t smem = (size_t)kWaves * entries * sizeof(uint64_t);
+  const bool block = any_block_scales(A);
+  void (*kern)(MultiArgs, int) = nullptr;
   switch (A.b[0].g.D) {  // (the caller checked that all batches share it)
-    case 64: hipLaunchKernelGGL(mfma_attention_kernel<64>, dim3(n_workgroups), dim3(kThreads), smem, s, A, entries); break;
-    case 128: hipLaunchKernelGGL(mfma_attention_kernel<128>, dim3(n_workgroups), dim3(kThreads), smem, s, A, entries); break;
-    default: hipLaunchKernelGGL(mfma_attention_kernel<256>, dim3(n_workgroups), dim3(kThreads), smem, s, A, entries); break;
+    case 64: kern = block ? mfma_block_attention_kernel<64> : mfma_attention_kernel<64>; break;
+    case 128: kern = block ? mfma_block_attention_kernel<128> : mfma_attention_kernel<128>; break;
+    default: kern = block ? mfma_block_attention_kernel<256> : mfma_attention_kernel<256>; break;
   }
+  hipLaunchKernelGGL(kern, dim3(n_workgroups), dim3(kThreads), smem, s, A, entries);
   return hipGetLastError();
 }
 
@@ -607,7 +641,9 @@ hipError_t launch_mfma_direct(const DirectArgs& args, hipStream_t s) {
   uint32_t* status = D.m.header + kHdrStatus;
   D.m.header += kHdrIgnored - kHdrStatus;
   static_assert(kThreads * ((uint64_t)kDirectMaxItems + 1) < 1ull << 32, "threads of the grid");
-  void (*const kern)(DirectArgs, uint32_t*) = hd == 64 ? mfma_direct_kernel<64> : hd == 128 ? mfma_direct_kernel<128> : mfma_direct_kernel<256>;
+  void (*kern)(DirectArgs, uint32_t*) = nullptr;
+  if (any_block_scales(D.m)) kern = hd == 64 ? mfma_block_direct_kernel<64> : hd == 128 ? mfma_block_direct_kernel<128> : mfma_block_direct_kernel<256>;
+  else kern = hd == 64 ? mfma_direct_kernel<64> : hd == 128 ? mfma_direct_kernel<128> : mfma_direct_kernel<256>;
   if (smem > 64 * 1024) {  // (head_dim 256 with 15 or 16 query heads per KV head: has to be granted per kernel)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != hipSuccess) return e;

@@ -24,6 +24,9 @@ struct Model {
   std::set<int32_t> partial_slabs;  // slabs of this key in PARTIAL state, ordered by id
   float* d_k_scale = nullptr;       // FP8: device [L][H]
   float* d_v_scale = nullptr;
+  uint64_t* d_turns = nullptr;  // rotary positions (fs_model_set_rope): device, turns per position of every pair in 2^-64
+  int rope_dim = 0, rope_layout = 0;
+  float rope_amplitude = 1.0f;
 };
 
 }  // namespace fs

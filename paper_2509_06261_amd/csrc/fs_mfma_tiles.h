@@ -20,7 +20,7 @@
 //   The head dimension decides the counts only: HD / 32 k-steps for S^T, HD / 16 output columns per lane (one
 //   16x16 accumulator tile each), HD / 16 elements of every V row per lane.
 //
-// Dequantization is folded around the MFMAs: FP8 static scales and INT8/INT4 per-token K scales
+// Dequantization is folded around the MFMAs (FP8_BLOCK's scales into the conversion of the codes): FP8 static scales and INT8/INT4 per-token K scales
 // multiply the logits, per-token V scales multiply P; integer codes enter the MFMA unconverted, as fp16
 // subnormals, and their offsets (128 for INT8, the zero-point for INT4) come back as rank-1
 // corrections (z_k * sum(q) on the logits, sum_t p_t s_t z_t on the output).
@@ -48,6 +48,10 @@ constexpr int kWaves = 4;
 constexpr int kD = 128;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+// Formats of E4M3 codes: they reach the MFMAs as fp16, FP8_BLOCK's multiplied by their block's scale (exactly: a power of two
+// in the range that keeps every value an fp16 number).
+template <int DT>
+constexpr bool e4m3_codes() { return DT == FS_KV_FP8_E4M3 || DT == FS_KV_FP8_BLOCK; }
 
 template <int DT, int HD = 128>
 struct Fmt {
@@ -129,8 +133,9 @@ __device__ __forceinline__ void static_for(std::integer_sequence<int, Is...>, F&
 //         operand carries 1/16 at those positions, the output columns are rescaled at the end.
 
 // two E4M3 bytes of a dword -> packed fp16 (exact)
-__device__ __forceinline__ uint32_t fp8x2_lo(uint32_t w) { return h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)); }
-__device__ __forceinline__ uint32_t fp8x2_hi(uint32_t w) { return h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)); }
+// (scale: a power of two; the conversion multiplies by it at no cost)
+__device__ __forceinline__ uint32_t fp8x2_lo(uint32_t w, float scale = 1.0f) { return h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false)); }
+__device__ __forceinline__ uint32_t fp8x2_hi(uint32_t w, float scale = 1.0f) { return h2u(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true)); }
 
 __device__ __forceinline__ void int8x4(uint32_t w, uint32_t& r0, uint32_t& r1) {
   const uint32_t u = w ^ 0x80808080u;
@@ -156,8 +161,20 @@ constexpr float kNoReference = -3.402823466e38f;
 
 // GP = padded group size: 4 when the KV head serves at most 4 query heads, else 16.  The MFMAs always work on 16
 // head columns; GP decides how the softmax between them is spread over the lanes (see softmax_pv).
+// FP8_BLOCK adds the scales of the K rows and of the V rows that the lane holds (a run lies in one block).
+template <int DT>
+struct TileScales {
+  __device__ __forceinline__ float k_scale() const { return 1.0f; }
+  __device__ __forceinline__ float v_scale() const { return 1.0f; }
+};
+template <>
+struct TileScales<FS_KV_FP8_BLOCK> {
+  float ks, vs;
+  __device__ __forceinline__ float k_scale() const { return ks; }
+  __device__ __forceinline__ float v_scale() const { return vs; }
+};
 template <int DT, int GP, int HD = 128>
-struct Tile {
+struct Tile : TileScales<DT> {
   typename KVec<Fmt<DT, HD>::kKLane>::type k[2][Fmt<DT, HD>::kKLoads];
   uint32_t v[8][Fmt<DT, HD>::kVWords];
   // INT8/INT4 per-token parameters.  GP == 16: one register; lanes c < 8 hold the K parameters of token c of
@@ -194,6 +211,7 @@ __device__ __forceinline__ void issue_k(const ItemCtx& X, int vb, int j, int c, 
   // row m = c of S^T tile u is slot 4u + (c & 3) of run c >> 2
   const RunLoc L = locate(X, vb, c >> 2);
   const gptr p = L.base + (uint32_t)((L.start + (c & 3)) * F::kRowBytes) + F::kKLane * j;
+  if constexpr (DT == FS_KV_FP8_BLOCK) t.ks = *reinterpret_cast<const FS_GLOBAL float*>(L.base + X.scale_off);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -213,7 +231,7 @@ __device__ __forceinline__ void issue_k(const ItemCtx& X, int vb, int j, int c, 
 template <int DT, int HD>
 constexpr bool wide_v() { return (DT == FS_KV_INT4 && HD == 128) || (DT == FS_KV_INT8 && HD == 64) || (DT == FS_KV_FP16 && HD == 256); }
 template <int DT, int HD, bool STREAM = false>
-constexpr bool nt_v() { return FS_NT_V && (DT == FS_KV_FP16 || DT == FS_KV_FP8_E4M3 || STREAM); }
+constexpr bool nt_v() { return FS_NT_V && (DT == FS_KV_FP16 || e4m3_codes<DT>() || STREAM); }
 // The output column that accumulator e of lane (j, c) holds: neighbours for e in steps of four, eight where HD > 64.
 template <int DT, int HD>
 __device__ __forceinline__ int column_of(int c, int e) {
@@ -275,6 +293,7 @@ template <int DT, int GP, int HD, bool WIDE = false, bool STREAM = false>
 __device__ __forceinline__ void issue_v(const ItemCtx& X, const DevGeom& g, int vb, int j, int c, Tile<DT, GP, HD>& t) {
   using F = Fmt<DT, HD>;
   const RunLoc L = locate(X, vb, j);
+  if constexpr (DT == FS_KV_FP8_BLOCK) t.vs = *reinterpret_cast<const FS_GLOBAL float*>(L.base + X.scale_off + 4);
   if constexpr (F::kParBytes != 0) {  // parameters first: the softmax needs them before the V rows
     const gptr pk = L.base + 2u * g.kv_tile;
     if constexpr (GP == 16) {
@@ -363,20 +382,20 @@ __device__ __forceinline__ float4v mfma(u32x4 a, u32x4 b, float4v acc) {
 // K fragments of one 16-token tile -> the A operands of S^T, one per k-step.
 template <int DT, int HD = 128>
 __device__ __forceinline__ void k_operands(const typename KVec<Fmt<DT, HD>::kKLane>::type (&k)[Fmt<DT, HD>::kKLoads],
-                                           u32x4 (&a)[HD / 32]) {
+                                           u32x4 (&a)[HD / 32], float scale = 1.0f) {
   constexpr int KS = HD / 32;
   if constexpr (DT == FS_KV_FP16) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) a[s] = k[s];
-  } else if constexpr (DT == FS_KV_FP8_E4M3) {
+  } else if constexpr (e4m3_codes<DT>()) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const u32x4 x = k[ks >> 1];
       const uint32_t w0 = x[2 * (ks & 1)], w1 = x[2 * (ks & 1) + 1];
-      a[ks][0] = fp8x2_lo(w0);
-      a[ks][1] = fp8x2_hi(w0);
-      a[ks][2] = fp8x2_lo(w1);
-      a[ks][3] = fp8x2_hi(w1);
+      a[ks][0] = fp8x2_lo(w0, scale);
+      a[ks][1] = fp8x2_hi(w0, scale);
+      a[ks][2] = fp8x2_lo(w1, scale);
+      a[ks][3] = fp8x2_hi(w1, scale);
     }
   } else if constexpr (DT == FS_KV_INT8) {
 #pragma unroll
@@ -411,7 +430,7 @@ __device__ __forceinline__ void k_operands(const typename KVec<Fmt<DT, HD>::kKLa
 // INT4: an odd column's elements are 16-fold.  (Left in the stored byte, 16 odd + even, for whoever reads the accumulators to take
 // the even column's sum off, they cost 32 instructions and 0.5 - 2 % less time, but an infinite weight then made NaN of Inf.)
 template <int DT, int HD, typename F>
-__device__ __forceinline__ void v_columns(const uint32_t (&v)[8][Fmt<DT, HD>::kVWords], F&& op) {
+__device__ __forceinline__ void v_columns(const uint32_t (&v)[8][Fmt<DT, HD>::kVWords], float scale, F&& op) {
   constexpr int NE = Fmt<DT, HD>::kNE;
   if constexpr (DT == FS_KV_FP16) {
     static_for(std::make_integer_sequence<int, NE>{}, [&](auto E) {
@@ -440,10 +459,10 @@ __device__ __forceinline__ void v_columns(const uint32_t (&v)[8][Fmt<DT, HD>::kV
       u32x4 b0, b1;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        if constexpr (DT == FS_KV_FP8_E4M3) {
+        if constexpr (e4m3_codes<DT>()) {
           const uint32_t x = __builtin_amdgcn_perm(v[2 * q + 1][e >> 2], v[2 * q][e >> 2], (e & 2) ? 0x07030602u : 0x05010400u);
-          b0[q] = fp8x2_lo(x);
-          b1[q] = fp8x2_hi(x);
+          b0[q] = fp8x2_lo(x, scale);
+          b1[q] = fp8x2_hi(x, scale);
         } else {
           const uint32_t x = __builtin_amdgcn_perm(v[2 * q + 1][e >> 3], v[2 * q][e >> 3], 0x0C040C00u + 0x00010001u * ((e & 7) >> 1));
           b0[q] = x & 0x000F000Fu;
@@ -466,16 +485,16 @@ __device__ __forceinline__ float column_value(const float4v (&acc)[NE], int e, i
 
 // One lane's elements of a V row -> packed-fp16 registers (layout note above).
 template <int DT, int HD = 128>
-__device__ __forceinline__ void v_unpack(const uint32_t (&v)[Fmt<DT, HD>::kVWords], uint32_t (&x)[Fmt<DT, HD>::kVRegs]) {
+__device__ __forceinline__ void v_unpack(const uint32_t (&v)[Fmt<DT, HD>::kVWords], uint32_t (&x)[Fmt<DT, HD>::kVRegs], float scale = 1.0f) {
   using F = Fmt<DT, HD>;
   if constexpr (DT == FS_KV_FP16) {
 #pragma unroll
     for (int p = 0; p < F::kVRegs; ++p) x[p] = v[p];
-  } else if constexpr (DT == FS_KV_FP8_E4M3) {
+  } else if constexpr (e4m3_codes<DT>()) {
 #pragma unroll
     for (int w = 0; w < F::kVWords; ++w) {
-      x[2 * w] = fp8x2_lo(v[w]);
-      x[2 * w + 1] = fp8x2_hi(v[w]);
+      x[2 * w] = fp8x2_lo(v[w], scale);
+      x[2 * w + 1] = fp8x2_hi(v[w], scale);
     }
   } else if constexpr (DT == FS_KV_INT8) {
 #pragma unroll
@@ -509,7 +528,7 @@ __device__ __forceinline__ void qk_tile(const Tile<DT, GP, HD>& t, const u32x4 (
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     u32x4 a[HD / 32];
-    k_operands<DT, HD>(t.k[u], a);
+    k_operands<DT, HD>(t.k[u], a, t.k_scale());
     float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < HD / 32; ++ks) acc = mfma(a[ks], qb[ks], acc);
@@ -577,7 +596,7 @@ __device__ __forceinline__ void softmax_pv(const ItemCtx& X, Tile<DT, GP, HD>& t
   const bool partial = !__all(L.lo == 0 && L.hi == 8);  // wave-uniform
   const uint32_t n_ok = (uint32_t)max(L.hi - L.lo, 0);  // of a partial tile: slot i of the run is live iff (unsigned)(i - lo) < n_ok
   if (partial) {
-    if constexpr (DT == FS_KV_FP16 || DT == FS_KV_FP8_E4M3) {
+    if constexpr (DT == FS_KV_FP16 || e4m3_codes<DT>()) {
       // slots past the sequence's end may hold NaN/Inf bit patterns; 0 * NaN would poison the MFMA
       // (slots before lo repeat live tokens: finite, their weight is 0)
 #pragma unroll
@@ -708,7 +727,7 @@ __device__ __forceinline__ void softmax_pv(const ItemCtx& X, Tile<DT, GP, HD>& t
   }
   // ---- V rows of the run -> B operands (8x8 in-register transpose) and out += P V ----
   if constexpr (DECODE && wide_v<DT, HD>() && DT != FS_KV_FP16) transpose_banks(t.v);
-  v_columns<DT, HD>(t.v, [&](auto E, const u32x4& b) { st.acc[decltype(E)::value] = mfma(pk, b, st.acc[decltype(E)::value]); });
+  v_columns<DT, HD>(t.v, t.v_scale(), [&](auto E, const u32x4& b) { st.acc[decltype(E)::value] = mfma(pk, b, st.acc[decltype(E)::value]); });
 }
 
 // Head-chunk addresses of blocks k0 .. k0 + nb - 1 of a sequence into this wave's LDS table: every lane of

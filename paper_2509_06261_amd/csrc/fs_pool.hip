@@ -33,7 +33,7 @@ static uint64_t layout(fs_geometry_t& g, int64_t tokens) {
   g.kv_tile = align_up((uint64_t)tokens * g.row_bytes, 16);
   g.par_tile = align_up((uint64_t)tokens * (uint64_t)g.param_bytes, 16);
   g.head_chunk = 2 * (g.kv_tile + g.par_tile);
-  g.layer_bytes = align_up((uint64_t)g.n_kv_heads * g.head_chunk, 256);
+  g.layer_bytes = align_up((uint64_t)g.n_kv_heads * (g.head_chunk + (g.kv_dtype == FS_KV_FP8_BLOCK ? 8 : 0)), 256);
   g.block_bytes = (uint64_t)g.n_layers * g.layer_bytes;
   g.tokens_per_block = (int32_t)tokens;
   return g.block_bytes;
@@ -119,6 +119,7 @@ int fs_pool_destroy(fs_pool* p) {
   for (auto& m : p->models) {
     if (m.d_k_scale) (void)hipFree(m.d_k_scale);
     if (m.d_v_scale) (void)hipFree(m.d_v_scale);
+    if (m.d_turns) (void)hipFree(m.d_turns);
   }
   if (p->owns_base) (void)hipFree(p->base);
   if (p->opt.ev0) (void)hipEventDestroy(p->opt.ev0);
@@ -133,7 +134,7 @@ void* fs_pool_base(fs_pool* p) { return p ? p->base : nullptr; }
 static int register_model(fs_pool* p, int kv_dtype, int n_kv_heads, int head_dim, int n_layers, uint64_t block_budget_bytes,
                           int forced_tokens, fs_model_t* out) {
   if (!p || !out) return FS_ERR_INVALID;
-  if (kv_dtype < FS_KV_FP16 || kv_dtype > FS_KV_INT4 || n_kv_heads < 1 || n_kv_heads > 1024 || n_layers < 1 ||
+  if (kv_dtype < FS_KV_FP16 || kv_dtype > FS_KV_FP8_BLOCK || n_kv_heads < 1 || n_kv_heads > 1024 || n_layers < 1 ||
       n_layers > 4096 || head_dim < 8 || head_dim > 512 || (head_dim & (head_dim - 1))) {
     set_error("fs_model_register: unsupported model shape");
     return FS_ERR_INVALID;
@@ -179,7 +180,7 @@ int fs_model_register_ex(fs_pool* p, int kv_dtype, int n_kv_heads, int head_dim,
 }
 
 static bool shape_ok(int kv_dtype, int n_kv_heads, int head_dim, int n_layers) {
-  return kv_dtype >= FS_KV_FP16 && kv_dtype <= FS_KV_INT4 && n_kv_heads >= 1 && n_kv_heads <= 1024 && n_layers >= 1 &&
+  return kv_dtype >= FS_KV_FP16 && kv_dtype <= FS_KV_FP8_BLOCK && n_kv_heads >= 1 && n_kv_heads <= 1024 && n_layers >= 1 &&
          n_layers <= 4096 && head_dim >= 8 && head_dim <= 512 && !(head_dim & (head_dim - 1));
 }
 
@@ -267,6 +268,7 @@ int fs_model_unregister(fs_pool* p, fs_model_t model) {
   }
   if (M->d_k_scale) (void)hipFree(M->d_k_scale);
   if (M->d_v_scale) (void)hipFree(M->d_v_scale);
+  if (M->d_turns) (void)hipFree(M->d_turns);
   *M = Model();
   return FS_OK;
 }

@@ -160,6 +160,7 @@ __device__ void prefill_item(const PrefillArgs& P, int seq, int head, int qt, ui
   X.len_u = first_pos + n_tok;                  // the tile's last query sees this many tokens
   X.len = live ? first_pos + tok_c + 1 : 1;     // causality: a column sees the tokens up to its own position
   X.chunk_ptr = s_ptr;
+  if constexpr (DT == FS_KV_FP8_BLOCK) X.scale_off = scale_offset(g, head);
 
   constexpr int NE = HD / 16;  // output columns NE c .. NE c + NE - 1 are this lane's
   u32x4 qb[HD / 32];
@@ -657,12 +658,12 @@ constexpr uint32_t stage_bytes(int subs, int hd = kD) { return stage_par(subs, h
 constexpr uint32_t kWgCtlBytes = 16;
 
 template <int DT, int HD>
-__device__ __forceinline__ void stage_k(uint8_t* stage, int sub, int lane, Tile<DT, 16, HD>& t) {  // (K fragments lead the stage)
+__device__ __forceinline__ void stage_k(uint8_t* stage, int sub, int lane, Tile<DT, 16, HD>& t, const uint32_t (&kpar)[2]) {  // (K fragments lead the stage)
   constexpr int KS = HD / 32;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     u32x4 a[KS];
-    k_operands<DT, HD>(t.k[u], a);
+    k_operands<DT, HD>(t.k[u], a, DT == FS_KV_FP8_BLOCK ? __uint_as_float(kpar[u]) : 1.0f);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
       *reinterpret_cast<u32x4*>(stage + (uint32_t)(((sub * 2 + u) * KS + ks) * kFrag) + lane * 16) = a[ks];
@@ -671,7 +672,7 @@ __device__ __forceinline__ void stage_k(uint8_t* stage, int sub, int lane, Tile<
 template <int DT, int SUBS, int HD>
 __device__ __forceinline__ void stage_v(uint8_t* stage, int sub, int lane, bool clear, int live, Tile<DT, 16, HD>& t) {
   using F = Fmt<DT, HD>;
-  if constexpr (DT == FS_KV_FP16 || DT == FS_KV_FP8_E4M3) {
+  if constexpr (DT == FS_KV_FP16 || e4m3_codes<DT>()) {
     // slots past the sequence's end may hold NaN/Inf bit patterns; 0 * NaN would poison the MFMA
     if (clear) {
 #pragma unroll
@@ -681,8 +682,12 @@ __device__ __forceinline__ void stage_v(uint8_t* stage, int sub, int lane, bool 
     }
   }
   uint32_t vx[8][F::kVRegs];
+  if constexpr (DT == FS_KV_FP8_BLOCK) {  // (slot i's scale: fetched by lane i of the row)
+    static_for(std::make_integer_sequence<int, 8>{}, [&](auto I) { v_unpack<DT, HD>(t.v[decltype(I)::value], vx[decltype(I)::value], row_bcast<decltype(I)::value>(t.vs)); });
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v_unpack<DT, HD>(t.v[i], vx[i]);
+    for (int i = 0; i < 8; ++i) v_unpack<DT, HD>(t.v[i], vx[i]);
+  }
 #pragma unroll
   for (int e = 0; e < F::kNE; ++e) {
     const int reg = DT == FS_KV_INT4 ? 4 * (e >> 3) + (e & 3) : (e >> 1);
@@ -765,6 +770,7 @@ __device__ __forceinline__ void dequant8(const uint32_t* w, const Deq<DT>& q, ui
 struct TokenCtx {
   const uint64_t* ptr;  // LDS: addresses of the blocks' layers from the segment's first block on
   uint64_t base_off;    // of the KV head
+  uint64_t scale_off;   // FP8_BLOCK: from the head's chunk to its scales
   int rel0;             // the segment's first token within its first block
   int last;             // the segment's last token, counted from its first one
   int T;
@@ -794,7 +800,9 @@ __device__ __forceinline__ void fetch_k(const TokenCtx& X, const DevGeom& g, boo
     const gptr at = p.base + (uint32_t)(p.slot * F::kRowBytes) + F::kKLane * j;
 #pragma unroll
     for (int s = 0; s < F::kKLoads; ++s) t.k[u][s] = *reinterpret_cast<const FS_GLOBAL kvec*>(at + 4 * F::kKLane * s);
-    if constexpr (PAR) {
+    if constexpr (DT == FS_KV_FP8_BLOCK) {
+      kpar[u] = *reinterpret_cast<const FS_GLOBAL uint32_t*>(p.base + X.scale_off);
+    } else if constexpr (PAR) {
       const gptr pp = p.base + 2u * g.kv_tile + (uint32_t)(p.slot * F::kParBytes);
       if constexpr (F::kParBytes == 2) kpar[u] = *reinterpret_cast<const FS_GLOBAL uint16_t*>(pp);
       else kpar[u] = *reinterpret_cast<const FS_GLOBAL uint32_t*>(pp);
@@ -821,6 +829,10 @@ __device__ __forceinline__ void fetch_v(const TokenCtx& X, const DevGeom& g, boo
   const int run = tb + 8 * j;
   const RunRows R = run_rows(X.rel0, X.last, X.T, X.magic, run, whole);
   const TokenPlace p{(gptr)(X.ptr[R.k] + X.base_off), R.k, R.slot};
+  if constexpr (DT == FS_KV_FP8_BLOCK) {  // lane c: the scale of token c % 8's block
+    const gptr base = whole ? p.base : place_token(X, min(run + (c & 7), X.last)).base;
+    t.vs = *reinterpret_cast<const FS_GLOBAL float*>(base + X.scale_off + 4);
+  }
   if constexpr (F::kParBytes != 0) {  // parameters first: they are needed before the rows
     TokenPlace o = p;
     if (whole) o.slot += c & 7;
@@ -1384,7 +1396,7 @@ __device__ void prefill_item_wg(const PrefillArgs& P, uint32_t* header, int seq,
   constexpr int CDT = DEQ ? FS_KV_FP16 : DT;  // the format the consumer code sees
   // V fragments read ahead of the softmax: what the format's register budget leaves room for (two waves per SIMD)
   // (eight instead of four: a 4 x 512-token FP8 chunk step 429.5 -> 423 us, INT8 prompts 817 -> 811 us; FP16 would spill)
-  constexpr int kVPre = NW != 8 ? 0 : (HD == kD && (DEQ || DT == FS_KV_FP8_E4M3) ? 8 : 4);
+  constexpr int kVPre = NW != 8 ? 0 : (HD == kD && (DEQ || e4m3_codes<DT>()) ? 8 : 4);
   const bool whole = P.whole_runs != 0;  // (uniform)
   const bool does_k = NW == SUBS || w < SUBS, does_v = NW == SUBS || w >= SUBS;  // wave-uniform staging roles
   const int sw = w % SUBS;                                                       // the sub-tile this wave stages
@@ -1416,6 +1428,7 @@ __device__ void prefill_item_wg(const PrefillArgs& P, uint32_t* header, int seq,
   TokenCtx X;
   X.ptr = s_tab;
   X.base_off = (uint64_t)head * g.head_chunk;
+  X.scale_off = DT == FS_KV_FP8_BLOCK ? scale_offset(g, head) : 0;
   X.T = g.T;
   X.magic = P.t_magic;
 
@@ -1478,7 +1491,7 @@ __device__ void prefill_item_wg(const PrefillArgs& P, uint32_t* header, int seq,
         if (does_k) stage_k_int<DT, HD>(stage, sw, lane, t, kpar);
         if (does_v) stage_v_int<DT, SUBS, HD>(stage, sw, lane, clear, live, alpha, t);
       } else {
-        if (does_k) stage_k<DT, HD>(stage, sw, lane, t);
+        if (does_k) stage_k<DT, HD>(stage, sw, lane, t, kpar);
         if (does_v) stage_v<DT, SUBS, HD>(stage, sw, lane, clear, live, t);
       }
     };
@@ -1735,7 +1748,8 @@ __device__ void prefill_item_wgp(const PrefillArgs& P, int seq, int head, int qt
     Tile<DT, 16> t;
     issue_k<DT, 16>(X, v0 + 4 * w, j, c, t);
     issue_v<DT, 16>(X, g, v0 + 4 * w, j, c, t);
-    stage_k<DT, kD>(smem, w, lane, t);
+    const uint32_t no_par[2] = {0u, 0u};
+    stage_k<DT, kD>(smem, w, lane, t, no_par);
     {
       const int live = locate(X, v0 + 4 * w, j).hi_u;
       stage_v<DT, SUBS, kD>(smem, w, lane, !__all(live >= 8), live, t);
@@ -1850,7 +1864,7 @@ __device__ void prefill_item_wgp(const PrefillArgs& P, int seq, int head, int qt
         }
       }
       uint8_t* next = smem + (uint32_t)((i + 1) & 1) * stage_bytes(SUBS);
-      stage_k<DT, kD>(next, w, lane, t);
+      stage_k<DT, kD>(next, w, lane, t, no_par);
       {
         const int live = locate(X, vb_next, j).hi_u;
         stage_v<DT, SUBS, kD>(next, w, lane, !__all(live >= 8), live, t);
@@ -1925,7 +1939,7 @@ constexpr int kBlocks256 = 4;    // ... and of its item at head_dim 256
 // (The walk without groups is up to 5 % slower in that kernel than in its own for FP8 and INT4 -- a prompt of 400 tokens 14.8 ->
 // 15.2, 15.8 -> 16.6 -- and the same for the others.)
 constexpr int group_context(int kv_shift, int dtype, bool d64, bool few_columns) {
-  if (kv_shift == 1) return dtype == FS_KV_FP16 ? 2048 : dtype == FS_KV_FP8_E4M3 ? 1536 : 1024;
+  if (kv_shift == 1) return dtype == FS_KV_FP16 ? 2048 : dtype == FS_KV_FP8_E4M3 || dtype == FS_KV_FP8_BLOCK ? 1536 : 1024;
   return !few_columns ? 640 : dtype == FS_KV_FP16 && !d64 ? 3072 : 1024;
 }
 constexpr int kSmallBlocks = 8;  // column blocks of the workgroup kernel's smaller item
@@ -2244,8 +2258,8 @@ __device__ __forceinline__ void direct_status(const PrefillArgs& P, uint32_t* s_
 
 // WPC = workgroups per compute unit the kernel is built for.  GROUPS: the groups' items, or -- where the scan finds no context
 // long enough -- those of the small launches' kernel, one block per wave.
-template <int DT, int NW, int NCB, int SUBS, int WPC, bool PIPE = false, bool DEQ = false, int HD = kD, bool SUM32 = false, bool GROUPS = false, bool SPLIT = false>
-__global__ __launch_bounds__(NW * 64, WPC) void prefill_wg_kernel(PrefillArgs P) {
+template <int DT, int NW, int NCB, int SUBS, bool PIPE, bool DEQ, int HD, bool SUM32, bool GROUPS, bool SPLIT>
+__device__ __forceinline__ void prefill_groups(const PrefillArgs& P) {
   extern __shared__ uint64_t smem64[];
   const DevBatch& B = P.b;
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem64);
@@ -2406,9 +2420,21 @@ __global__ __launch_bounds__(NW * 64, WPC) void prefill_wg_kernel(PrefillArgs P)
 #endif
 }
 
+template <int DT, int NW, int NCB, int SUBS, int WPC, bool PIPE = false, bool DEQ = false, int HD = kD, bool SUM32 = false, bool GROUPS = false, bool SPLIT = false>
+__global__ __launch_bounds__(NW * 64, WPC) void prefill_wg_kernel(PrefillArgs P) {
+  prefill_groups<DT, NW, NCB, SUBS, PIPE, DEQ, HD, SUM32, GROUPS, SPLIT>(P);
+}
+// FP8_BLOCK models.  (Sums over the unrounded weights everywhere: lse is then exact to fp32's sums; four chunks of 512 behind 3000 -
+// 16384 tokens take 312 us like this and 317 with the sums of the rounded ones.)
+template <int NW, int NCB, int SUBS, int HD, bool GROUPS = false, bool SPLIT = false>
+__global__ __launch_bounds__(NW * 64, 1) void prefill_wg_block_kernel(PrefillArgs P) {
+  prefill_groups<FS_KV_FP8_BLOCK, NW, NCB, SUBS, false, false, HD, true, GROUPS, SPLIT>(P);
+}
+
 // The 16-column kernel (HD: its tile code takes any of the three head_dims).
-template <int HD>
-__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void prefill_kernel(PrefillArgs P) {
+// BLOCK: FP8_BLOCK models, in a kernel of their own.
+template <int HD, bool BLOCK>
+__device__ __forceinline__ void prefill_columns(const PrefillArgs& P) {
   extern __shared__ uint64_t smem64[];
   const DevBatch& B = P.b;
   const int lane = threadIdx.x & 63;
@@ -2420,13 +2446,23 @@ __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void prefill_kernel(
   for (uint32_t item; next_item(d, P.header, total, kWaveChunkShift, lane, item);) {
     int seq, head, qt;
     if (!decode_item(P, P.tile_first, item, H, seq, head, qt)) continue;
-    switch (B.g.dtype) {
+    if constexpr (BLOCK) prefill_item<FS_KV_FP8_BLOCK, HD>(P, seq, head, qt, s_ptr);
+    else switch (B.g.dtype) {
       case FS_KV_FP16: prefill_item<FS_KV_FP16, HD>(P, seq, head, qt, s_ptr); break;
       case FS_KV_FP8_E4M3: prefill_item<FS_KV_FP8_E4M3, HD>(P, seq, head, qt, s_ptr); break;
       case FS_KV_INT8: prefill_item<FS_KV_INT8, HD>(P, seq, head, qt, s_ptr); break;
       default: prefill_item<FS_KV_INT4, HD>(P, seq, head, qt, s_ptr); break;
     }
   }
+}
+
+template <int HD>
+__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void prefill_kernel(PrefillArgs P) {
+  prefill_columns<HD, false>(P);
+}
+template <int HD>
+__global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void prefill_block_kernel(PrefillArgs P) {
+  prefill_columns<HD, true>(P);
 }
 
 uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
@@ -2487,7 +2523,9 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
   const int tpt = 16 / G;
   // (FS_OPT_PREFILL_COLUMN_BLOCKS chooses among variants that are built for head_dim 128: one setting for a pool must not
   // take its models of head_dim 64 and 256 off the kernel that suits their launches)
-  const int ncb_env = g.head_dim == kD ? p->opt.prefill_ncb : 0;
+  // (nor are they built for FP8_BLOCK models)
+  const bool block = g.kv_dtype == FS_KV_FP8_BLOCK;
+  const int ncb_env = g.head_dim == kD && !block ? p->opt.prefill_ncb : 0;
   // the wide kernels fold the (positive) softmax scale into the exponential's argument; any other scale takes
   // the 16-column kernel, which does not
   const bool scale_ok = sm_scale > 0.f && sm_scale < INFINITY;
@@ -2628,7 +2666,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
   // library's own choice keeps the integer codes exact and its sums over the unrounded weights, as the 16-column kernel that
   // served it before, and the 4-wave kernels are not built like that)
   const bool large = ncb_env || items >= (uint64_t)p->n_cu;
-  const int nw = d256 || (p->opt.prefill_nw == 4 && ncb == 16 && !d64 && large) ? 4 : 8;
+  const int nw = d256 || (p->opt.prefill_nw == 4 && ncb == 16 && !d64 && large && !block) ? 4 : 8;
   // the workgroups list the sequences themselves while they have a thread for each; the per-sequence tile counts of more
   // go to LDS while they fit beside the stages (16 KiB: 4095 sequences)
   P.tf_cache = !wg || generic ? 0 : (nw == 8 || d256) && n_seq <= nw * 64 ? 2 : (uint64_t)n_seq + 1 <= 4096;
@@ -2637,7 +2675,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
   // Split items: up to four of 16 blocks per compute unit (the queue deals more as evenly: 3 prompts of 2000 - 6000 tokens, 3.8 per
   // unit, 509 us with either), where the tables can hold eight steps (the workgroups, who see the lengths, decide: see lay_plan)
   // and the workspace has room for the pieces.
-  const bool deq_on = p->opt.prefill_deq || g.kv_dtype == FS_KV_FP16 || g.kv_dtype == FS_KV_FP8_E4M3;
+  const bool deq_on = p->opt.prefill_deq || (g.kv_dtype != FS_KV_INT8 && g.kv_dtype != FS_KV_INT4);
   const uint32_t split_groups = std::min<uint32_t>(kSplitGroups, (uint32_t)p->n_cu & ~7u);
   const int64_t capacity = std::min<int64_t>((int64_t)max_blocks * g.tokens_per_block, 0x7fffffff);
   bool split = P.tf_cache == 2 && g.head_dim == kD && nw == 8 && ncb == 16 && !ncb_env && large && deq_on && split_groups >= 8 &&
@@ -2712,6 +2750,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
       switch (g.kv_dtype) {
         case FS_KV_FP16: kern = prefill_wg_kernel<FS_KV_FP16, 4, 1, 2, 1, false, false, 256, true>; break;
         case FS_KV_FP8_E4M3: kern = prefill_wg_kernel<FS_KV_FP8_E4M3, 4, 1, 2, 1, false, false, 256, true>; break;
+        case FS_KV_FP8_BLOCK: kern = prefill_wg_block_kernel<4, 1, 2, 256>; break;
         case FS_KV_INT8: kern = prefill_wg_kernel<FS_KV_INT8, 4, 1, 2, 1, false, false, 256, true>; break;
         default: kern = prefill_wg_kernel<FS_KV_INT4, 4, 1, 2, 1, false, false, 256, true>; break;
       }
@@ -2721,6 +2760,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
       switch (g.kv_dtype) {
         case FS_KV_FP16: kern = FS_WGKV(FS_KV_FP16); break;
         case FS_KV_FP8_E4M3: kern = FS_WGKV(FS_KV_FP8_E4M3); break;
+        case FS_KV_FP8_BLOCK: kern = d64 ? prefill_wg_block_kernel<8, 2, 4, 64, true> : prefill_wg_block_kernel<8, 2, 4, kD, true>; break;
         case FS_KV_INT8: kern = FS_WGKV(FS_KV_INT8); break;
         default: kern = FS_WGKV(FS_KV_INT4); break;
       }
@@ -2732,6 +2772,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
       switch (g.kv_dtype) {
         case FS_KV_FP16: kern = FS_WG1(FS_KV_FP16); break;
         case FS_KV_FP8_E4M3: kern = FS_WG1(FS_KV_FP8_E4M3); break;
+        case FS_KV_FP8_BLOCK: kern = d64 ? prefill_wg_block_kernel<8, 1, 4, 64> : prefill_wg_block_kernel<8, 1, 4, kD>; break;
         case FS_KV_INT8: kern = FS_WG1(FS_KV_INT8); break;
         default: kern = FS_WG1(FS_KV_INT4); break;
       }
@@ -2743,6 +2784,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
       switch (g.kv_dtype) {
         case FS_KV_FP16: kern = FS_WG64(FS_KV_FP16, 4); break;
         case FS_KV_FP8_E4M3: kern = FS_WG64(FS_KV_FP8_E4M3, 3); break;
+        case FS_KV_FP8_BLOCK: kern = ncb == 16 ? prefill_wg_block_kernel<8, 2, 4, 64> : prefill_wg_block_kernel<8, 3, 4, 64>; break;
         case FS_KV_INT8: kern = FS_WG64(FS_KV_INT8, 3); break;
         default: kern = FS_WG64(FS_KV_INT4, 3); break;
       }
@@ -2752,6 +2794,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
       switch (g.kv_dtype) {
         case FS_KV_FP16: kern = FS_WGS(FS_KV_FP16, false); break;
         case FS_KV_FP8_E4M3: kern = FS_WGS(FS_KV_FP8_E4M3, false); break;
+        case FS_KV_FP8_BLOCK: kern = prefill_wg_block_kernel<8, 2, 4, kD, false, true>; break;
         case FS_KV_INT8: kern = FS_WGS(FS_KV_INT8, true); break;
         default: kern = FS_WGS(FS_KV_INT4, true); break;
       }
@@ -2759,6 +2802,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
     } else switch (g.kv_dtype) {
       case FS_KV_FP16: kern = large ? FS_WG(FS_KV_FP16) : prefill_wg_kernel<FS_KV_FP16, 8, 2, 4, 1, false, false, kD, true>; break;
       case FS_KV_FP8_E4M3: kern = large ? FS_WG(FS_KV_FP8_E4M3) : prefill_wg_kernel<FS_KV_FP8_E4M3, 8, 2, 4, 1, false, false, kD, true>; break;
+      case FS_KV_FP8_BLOCK: kern = prefill_wg_block_kernel<8, 2, 4, kD>; break;
       case FS_KV_INT8: kern = deq ? prefill_wg_kernel<FS_KV_INT8, 8, 2, 4, 1, false, true> : FS_WG(FS_KV_INT8); break;
       default: kern = deq ? prefill_wg_kernel<FS_KV_INT4, 8, 2, 4, 1, false, true> : FS_WG(FS_KV_INT4); break;
     }
@@ -2771,9 +2815,11 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
     hipLaunchKernelGGL(kern, dim3(n_wg), dim3(nw * 64), smem, s, P);
   } else if (ncb == 1) {
     p->opt.last_prefill = 1;
-    if (g.head_dim == 64) hipLaunchKernelGGL(prefill_kernel<64>, dim3(n_wg), dim3(kThreads), smem, s, P);
-    else if (g.head_dim == 256) hipLaunchKernelGGL(prefill_kernel<256>, dim3(n_wg), dim3(kThreads), smem, s, P);
-    else hipLaunchKernelGGL(prefill_kernel<kD>, dim3(n_wg), dim3(kThreads), smem, s, P);
+    void (*kern)(PrefillArgs) = nullptr;
+    if (g.head_dim == 64) kern = block ? prefill_block_kernel<64> : prefill_kernel<64>;
+    else if (g.head_dim == 256) kern = block ? prefill_block_kernel<256> : prefill_kernel<256>;
+    else kern = block ? prefill_block_kernel<kD> : prefill_kernel<kD>;
+    hipLaunchKernelGGL(kern, dim3(n_wg), dim3(kThreads), smem, s, P);
   } else {
     void (*kern)(PrefillArgs) = nullptr;
 #define FS_WIDE(DT) (ncb == 4 ? prefill_wide_kernel<DT, 4, 1> : prefill_wide_kernel<DT, 2, 1>)
