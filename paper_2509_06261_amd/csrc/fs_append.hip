@@ -6,6 +6,12 @@
 
 #include "fs_append_block.h"
 
+#ifndef FS_X_HEADS
+#define FS_X_HEADS 4
+#endif
+#ifndef FS_X_TEAMS
+#define FS_X_TEAMS 8
+#endif
 namespace fs {
 namespace {
 
@@ -20,10 +26,15 @@ __global__ __launch_bounds__(kWaves * 64) void kv_append_kernel(AppendArgs A) {
   append_rows<kSrcF32, DT, HP>(A, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves);
 }
 
-template <bool kSrcF32>
-__global__ __launch_bounds__(kWaves * 64) void kv_append_block_kernel(AppendArgs A) {
-  __shared__ float s_max[kWaves];
-  append_groups<kSrcF32, false, kWaves>(A, rope::RopeArgs{}, blockIdx.x, gridDim.x, s_max);
+// FP8_BLOCK models.  TEAM: waves that work on a group together.
+template <bool kSrcF32, int TEAM, bool LATE, bool SINGLES>
+__global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64) void kv_append_block_kernel(AppendArgs A, int heads) {
+  if constexpr (TEAM == 1) {
+    append_groups<kSrcF32, kPlain, 1, LATE, SINGLES>(A, rope::RopeArgs{}, heads, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves, nullptr, nullptr);
+  } else {
+    __shared__ float s_max[2 * TEAM];
+    append_groups<kSrcF32, kPlain, TEAM, LATE, SINGLES>(A, rope::RopeArgs{}, heads, blockIdx.x, gridDim.x, s_max, nullptr);
+  }
 }
 
 template <bool BLOCK>
@@ -87,6 +98,24 @@ static int64_t append_units(const append::AppendArgs& A, int hp) {
   return (A.n_tokens + tpw - 1) / tpw * ((2 * (int64_t)A.g.H + hp - 1) / hp);
 }
 
+append::GroupPlan plan_groups(const fs_pool* p, const append::AppendArgs& A) {
+  const int H = A.g.H;
+  const int64_t most = (int64_t)p->n_cu * 64;
+  append::GroupPlan G{};
+  const int held = (64 >> A.lpr_shift) * append::kSteps;  // rows that a wave keeps
+  G.team = A.g.T <= held ? 1 : A.g.T <= 4 * held ? 4 : 8;
+  G.late = A.g.T > 8 * held;
+  G.singles = A.n_tokens <= 8192;
+  // several heads to a unit where whole blocks of tokens make enough units
+  const int64_t groups = std::max<int64_t>(A.n_tokens / A.g.T, 1), full = (int64_t)p->n_cu * 8 / G.team;
+  G.heads = (int)std::min<int64_t>(std::min(H, FS_X_HEADS), std::max<int64_t>(groups * 2 * H / full, 1));
+  const int parts = 2 * ((H + G.heads - 1) / G.heads);
+  G.chunk = group_chunk(A.n_tokens, parts, (int64_t)p->n_cu * FS_X_TEAMS);
+  const int64_t units = (A.n_tokens + G.chunk - 1) / G.chunk * parts;
+  G.blocks = std::min(G.team > 1 ? units : (units + kWaves - 1) / kWaves, most);
+  return G;
+}
+
 uint32_t plan_append_blocks(const fs_pool* p, append::MultiAppendArgs& P, int waves) {
   const int64_t cap = std::max<int64_t>((int64_t)p->n_cu * 64 * 4 / waves, 1);  // per append: as the single-append launch
   uint32_t next = 0;
@@ -130,12 +159,17 @@ extern "C" int fs_kv_append(fs_pool* p, fs_model_t model, int layer, const void*
     set_error("fs_kv_append: pool has no HIP device");
     return FS_ERR_DEVICE;
   }
-  if (A.g.dtype == FS_KV_FP8_BLOCK) {  // a workgroup for every unit
-    A.group_chunk = group_chunk(n_tokens, 2 * A.g.H, (int64_t)p->n_cu * 8);
-    const int64_t teams = std::min<int64_t>(append_units(A, 1), (int64_t)p->n_cu * 64);
+  if (A.g.dtype == FS_KV_FP8_BLOCK) {
+    const append::GroupPlan G = plan_groups(p, A);
+    A.group_chunk = G.chunk;
+    void (*kern)(AppendArgs, int) = nullptr;
+#define FS_APPEND(TEAM, LATE)                                                                                                   \
+  (G.singles ? (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE, true> : kv_append_block_kernel<false, TEAM, LATE, true>)   \
+             : (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE, false> : kv_append_block_kernel<false, TEAM, LATE, false>))
+    kern = G.late ? FS_APPEND(8, true) : G.team == 8 ? FS_APPEND(8, false) : G.team == 4 ? FS_APPEND(4, false) : FS_APPEND(1, false);
+#undef FS_APPEND
     (void)hipGetLastError();
-    hipLaunchKernelGGL(A.src_f32 ? kv_append_block_kernel<true> : kv_append_block_kernel<false>, dim3((unsigned)teams), dim3(kWaves * 64), 0,
-                       (hipStream_t)stream, A);
+    hipLaunchKernelGGL(kern, dim3((unsigned)G.blocks), dim3((G.team > 1 ? G.team : kWaves) * 64), 0, (hipStream_t)stream, A, G.heads);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return device_error(e, "fs_kv_append launch");
     return FS_OK;

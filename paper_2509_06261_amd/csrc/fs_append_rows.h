@@ -189,15 +189,32 @@ __device__ __forceinline__ void load8(const void* src, int64_t idx, float (&x)[k
 // divisions for a row's place, was bound by the vector ALU: 328 instructions per four rows, 65 600 fp32 tokens x 8
 // heads -> INT4 in 157 us (3.9 TB/s).  Now about 100 instructions and 130 us (4.7 TB/s, a plain copy moves 4.3); FP16
 // -> FP8 154 -> 69 us, FP16 -> FP16 117 -> 79 us.
-template <int DT>
+// SPLIT: they are not eight neighbours but the four from `da` and the four from `db` on.
+template <int DT, bool SPLIT = false>
 __device__ __forceinline__ void quantize_row(const float (&x)[kEpl], bool ok, uint8_t* row, uint8_t* par, float sc, int lir,
-                                             int lpr) {
+                                             int lpr, int da = 0, int db = 0) {
   const int d0 = lir * kEpl;  // this lane's first element (head_dim >= 8: always inside the row)
+  // the lane's codes: bytes of four elements at a time
+  auto put8 = [&](const u32x2& w) {
+    if constexpr (SPLIT) {
+      kv_store(reinterpret_cast<uint32_t*>(row + da), w[0]);
+      kv_store(reinterpret_cast<uint32_t*>(row + db), w[1]);
+    } else {
+      kv_store(reinterpret_cast<u32x2*>(row + d0), w);
+    }
+  };
   if constexpr (DT == FS_KV_FP16) {
     u32x4 w;
 #pragma unroll
     for (int q = 0; q < 4; ++q) w[q] = (uint32_t)f16_bits(x[2 * q]) | ((uint32_t)f16_bits(x[2 * q + 1]) << 16);
-    if (ok) kv_store(reinterpret_cast<u32x4*>(row + 2 * d0), w);
+    if (ok) {
+      if constexpr (SPLIT) {
+        kv_store(reinterpret_cast<u32x2*>(row + 2 * da), u32x2{w[0], w[1]});
+        kv_store(reinterpret_cast<u32x2*>(row + 2 * db), u32x2{w[2], w[3]});
+      } else {
+        kv_store(reinterpret_cast<u32x4*>(row + 2 * d0), w);
+      }
+    }
   } else if constexpr (DT == FS_KV_FP8_E4M3) {
     u32x2 w = {0u, 0u};
     if (sc >= 0x1p-40f && sc <= 0x1p40f) {
@@ -216,7 +233,7 @@ __device__ __forceinline__ void quantize_row(const float (&x)[kEpl], bool ok, ui
 #pragma unroll
       for (int q = 0; q < kEpl; ++q) w[q >> 2] |= e4m3_bits(__fdiv_rn(x[q], sc)) << (8 * (q & 3));
     }
-    if (ok) kv_store(reinterpret_cast<u32x2*>(row + d0), w);
+    if (ok) put8(w);
   } else if constexpr (DT == FS_KV_INT8) {
     float amax = 0.f;
 #pragma unroll
@@ -237,7 +254,7 @@ __device__ __forceinline__ void quantize_row(const float (&x)[kEpl], bool ok, ui
       w[h] = s ^ 0x80808080u;
     }
     if (ok) {
-      kv_store(reinterpret_cast<u32x2*>(row + d0), w);
+      put8(w);
       if (lir == 0) *reinterpret_cast<uint16_t*>(par) = sb;
     }
   } else {  // FS_KV_INT4
@@ -262,7 +279,12 @@ __device__ __forceinline__ void quantize_row(const float (&x)[kEpl], bool ok, ui
       w += __float_as_uint(c + kRound) << (4 * q);
     }
     if (ok) {
-      kv_store(reinterpret_cast<uint32_t*>(row + (d0 >> 1)), w);
+      if constexpr (SPLIT) {
+        kv_store(reinterpret_cast<uint16_t*>(row + (da >> 1)), (uint16_t)w);
+        kv_store(reinterpret_cast<uint16_t*>(row + (db >> 1)), (uint16_t)(w >> 16));
+      } else {
+        kv_store(reinterpret_cast<uint32_t*>(row + (d0 >> 1)), w);
+      }
       if (lir == 0) *reinterpret_cast<uint32_t*>(par) = (uint32_t)sb | ((uint32_t)f16_bits(z) << 16);
     }
   }

@@ -30,41 +30,37 @@ struct TurnArgs {
 
 // A unit: HP neighbouring heads of 64 / lpr consecutive tokens, a token's row per lpr lanes.  A row lies in one wave, which
 // reads all of it before it writes: `out` may be `x`.
-template <bool kF32, int HP>
-__device__ __forceinline__ void turn_rows(const TurnArgs& A, int64_t worker, int64_t n_workers) {
-  const int lane = threadIdx.x & 63;
-  const int tpw = 64 >> A.lpr_shift, d0 = (lane & ((1 << A.lpr_shift) - 1)) * kEpl;
-  const LaneTurns turns = lane_turns(A.rope, d0);
+template <int MODE, bool kF32, bool kOutF32, int HP>
+__global__ __launch_bounds__(kWaves * 64) void turn_kernel(TurnArgs A) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tpw = 64 >> A.lpr_shift;
+  const Lane L = lane_of<MODE>(A.rope, lane & ((1 << A.lpr_shift) - 1));
+  const Turns<MODE> turns = lane_turns<MODE>(A.rope, L);
   const uint32_t parts = (uint32_t)(A.n_heads + HP - 1) / HP;
   const int64_t n_units = (A.n_tokens + tpw - 1) / tpw * parts;
-  for (int64_t unit = worker; unit < n_units; unit += n_workers) {
-    const int64_t grp = unit / parts;
-    const int h0 = (int)(unit % parts) * HP;
+  for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < n_units; unit += (int64_t)gridDim.x * kWaves) {
+    int64_t grp;
+    int h0;
+    split_unit(unit, parts, grp, h0);
+    h0 *= HP;
     const int64_t tok = grp * tpw + (lane >> A.lpr_shift);
-    const int pos = tok < A.n_tokens ? A.pos[tok] : -1;
-    const bool ok = pos >= 0;  // (a negative position: padding, its row of out stays as it is)
-    float x[HP][kEpl], y[HP][kEpl];
+    const bool in = tok < A.n_tokens;
+    auto row = [&](int k) { return tok * A.x_stride + (int64_t)(h0 + k) * A.d; };
+    Raw<kF32> w[HP];
+#pragma unroll
+    for (int k = 0; k < HP; ++k)
+      if (in && h0 + k < A.n_heads) load_raw<kF32, MODE == kSplit>(A.x, row(k), L, w[k]);
+    const int pos = in ? A.pos[tok] : -1;  // (negative: padding, its row of out stays as it is)
+    const Factors<MODE> F = factors<MODE>(A.rope, L, turns, max(pos, 0));
 #pragma unroll
     for (int k = 0; k < HP; ++k) {
-      if (!ok || h0 + k >= A.n_heads) continue;
-      const int64_t row = tok * A.x_stride + (int64_t)(h0 + k) * A.d;
-      load8<kF32>(A.x, row + d0, x[k]);
-      if (!A.rope.pairs && turns.live) load_partners<kF32>(A.x, row, turns, A.rope.dim, y[k]);
-    }
-    const Factors F = factors(A.rope, turns, max(pos, 0));
-#pragma unroll
-    for (int k = 0; k < HP; ++k) {
-      if (!ok || h0 + k >= A.n_heads) continue;
-      if (turns.live) turn_row(A.rope, turns, F, x[k], y[k]);
-      store8<kF32>(A.out, tok * A.out_stride + (int64_t)(h0 + k) * A.d + d0, x[k]);
+      if (pos < 0 || h0 + k >= A.n_heads) continue;
+      float x[kEpl];
+      widen<kF32>(w[k], x);
+      turn_row<MODE, kF32>(A.rope, L, F, x, A.x, row(k));
+      store8<kOutF32, MODE == kSplit>(A.out, tok * A.out_stride + (int64_t)(h0 + k) * A.d, L, x);
     }
   }
-}
-
-template <bool kF32, int HP>
-__global__ __launch_bounds__(kWaves * 64) void turn_kernel(TurnArgs A) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  turn_rows<kF32, HP>(A, (int64_t)blockIdx.x * kWaves + wave, (int64_t)gridDim.x * kWaves);
 }
 
 // ---- fs_rope_append -----------------------------------------------------------------------------------------------
@@ -87,38 +83,42 @@ __device__ __forceinline__ uint8_t* token_layer(const AppendArgs& A, const Token
 }
 
 // Rows k0 .. k0 + HP - 1 of a token's n_q query heads, H key heads and H value heads.  CACHE = false: of its query heads alone.
-template <bool kSrcF32, int DT, int HP, bool CACHE>
+template <int MODE, bool kSrcF32, int DT, int HP, bool CACHE>
 __device__ __forceinline__ void rope_append_rows(const RopeAppendArgs& P, int64_t worker, int64_t n_workers) {
   const AppendArgs& A = P.a;
   const DevGeom& g = A.g;
   const int lane = threadIdx.x & 63;
-  const int lpr = 1 << A.lpr_shift, tpw = 64 >> A.lpr_shift, lir = lane & (lpr - 1), d0 = lir * kEpl;
-  const LaneTurns turns = lane_turns(P.rope, d0);
+  const int lpr = 1 << A.lpr_shift, tpw = 64 >> A.lpr_shift, lir = lane & (lpr - 1);
+  const Lane L = lane_of<MODE>(P.rope, lir), plain{kEpl * lir, kEpl * lir + 4, 0, 0, false};
+  const Turns<MODE> turns = lane_turns<MODE>(P.rope, L);
   const int rows = P.n_q + (CACHE ? 2 * g.H : 0), turned = P.n_q + (CACHE ? g.H : 0);
   const uint32_t parts = (uint32_t)(rows + HP - 1) / HP;
   const int64_t n_units = (A.n_tokens + tpw - 1) / tpw * parts;
   for (int64_t unit = worker; unit < n_units; unit += n_workers) {
-    const int64_t grp = unit / parts;
-    const int k0 = (int)(unit % parts) * HP;
+    int64_t grp;
+    int k0;
+    split_unit(unit, parts, grp, k0);
+    k0 *= HP;
     const int64_t tok = grp * tpw + (lane >> A.lpr_shift);
     const bool in = tok < A.n_tokens;
-    float x[HP][kEpl], y[HP][kEpl];
+    auto source = [&](int r, const void*& src) {  // where row r begins (r is uniform)
+      const bool is_q = r < P.n_q, is_k = r < turned;
+      src = is_q ? P.q : is_k ? A.k_new : A.v_new;
+      return tok * (is_q ? P.q_stride : is_k ? A.k_stride : A.v_stride) + (int64_t)(is_q ? r : is_k ? r - P.n_q : r - turned) * g.D;
+    };
+    Raw<kSrcF32> w[HP];
 #pragma unroll
     for (int k = 0; k < HP; ++k) {
-#pragma unroll
-      for (int q = 0; q < kEpl; ++q) x[k][q] = y[k][q] = 0.f;
-      const int r = k0 + k;  // (uniform)
+      const int r = k0 + k;
       if (!in || r >= rows) continue;
-      const bool is_q = r < P.n_q, is_k = !is_q && r < turned;
-      const void* const src = is_q ? P.q : is_k ? A.k_new : A.v_new;
-      const int head = is_q ? r : is_k ? r - P.n_q : r - turned;
-      const int64_t row = tok * (is_q ? P.q_stride : is_k ? A.k_stride : A.v_stride) + (int64_t)head * g.D;
-      load8<kSrcF32>(src, row + d0, x[k]);
-      if (r < turned && !P.rope.pairs && turns.live) load_partners<kSrcF32>(src, row, turns, P.rope.dim, y[k]);
+      const void* src;
+      const int64_t row = source(r, src);
+      if (r < turned) load_raw<kSrcF32, MODE == kSplit>(src, row, L, w[k]);
+      else load_raw<kSrcF32, false>(src, row, plain, w[k]);
     }
     const int pos = in ? A.pos[tok] : -1;
-    Factors F{};
-    if (k0 < turned) F = factors(P.rope, turns, max(pos, 0));
+    Factors<MODE> F{};
+    if (k0 < turned) F = factors<MODE>(P.rope, L, turns, max(pos, 0));
     TokenKey key{-1, 0, 0};
     uint8_t* layer = nullptr;
     if (CACHE && k0 + HP > P.n_q) {
@@ -129,36 +129,80 @@ __device__ __forceinline__ void rope_append_rows(const RopeAppendArgs& P, int64_
     for (int k = 0; k < HP; ++k) {
       const int r = k0 + k;
       if (r >= rows) break;
-      if (r < turned && turns.live) turn_row(P.rope, turns, F, x[k], y[k]);
+      float x[kEpl] = {};
+      if (in) {
+        widen<kSrcF32>(w[k], x);
+        if (r < turned) {
+          const void* src;
+          const int64_t row = source(r, src);
+          turn_row<MODE, kSrcF32>(P.rope, L, F, x, src, row);
+        }
+      }
       if (r < P.n_q) {
-        if (pos >= 0) store8<false>(P.q_out, (tok * P.n_q + r) * (int64_t)g.D + d0, x[k]);
+        if (pos >= 0) store8<false, MODE == kSplit>(P.q_out, (tok * P.n_q + r) * (int64_t)g.D, L, x);
       } else if constexpr (CACHE) {
         const int which = r >= turned, head = which ? r - turned : r - P.n_q;
         uint8_t* const chunk = layer + (uint64_t)head * g.head_chunk;
         uint8_t* const row = chunk + (which ? g.kv_tile : 0u) + (uint64_t)key.slot * g.row_bytes;
         uint8_t* const par = chunk + 2u * g.kv_tile + (which ? g.par_tile : 0u) + (uint64_t)key.slot * (uint32_t)g.param_bytes;
         const float sc = DT == FS_KV_FP8_E4M3 ? (which ? A.v_scale : A.k_scale)[head] : 1.0f;
-        quantize_row<DT>(x[k], layer != nullptr, row, par, sc, lir, lpr);
+        if (MODE == kSplit && !which) quantize_row<DT, true>(x, layer != nullptr, row, par, sc, lir, lpr, L.a, L.b);
+        else quantize_row<DT>(x, layer != nullptr, row, par, sc, lir, lpr);
       }
     }
   }
 }
 
-template <bool kSrcF32, int DT, int HP>
+template <int MODE, bool kSrcF32, int DT, int HP>
 __global__ __launch_bounds__(kWaves * 64) void rope_append_kernel(RopeAppendArgs P) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  rope_append_rows<kSrcF32, DT, HP, true>(P, (int64_t)blockIdx.x * kWaves + wave, (int64_t)gridDim.x * kWaves);
+  rope_append_rows<MODE, kSrcF32, DT, HP, true>(P, (int64_t)blockIdx.x * kWaves + wave, (int64_t)gridDim.x * kWaves);
 }
 
-// FP8_BLOCK: the keys and values by groups of a block's tokens (fs_append_block.h), the queries by rows.
-template <bool kSrcF32, int HP>
-__global__ __launch_bounds__(kWaves * 64) void rope_append_block_kernel(RopeAppendArgs P) {
-  __shared__ float s_max[kWaves];
+// FP8_BLOCK: the keys and values by groups of a block's tokens (fs_append_block.h), the queries by rows.  The cache's workgroups
+// come first: they take longest.  TEAM, heads: as in kv_append_block_kernel.  Dynamic LDS: the teams' tables of angles.
+template <int MODE, bool kSrcF32, int TEAM, bool LATE, bool SINGLES>
+__global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64) void rope_append_block_kernel(RopeAppendArgs P, int heads) {
+  extern __shared__ float s_table[];
+  constexpr int kOwn = TEAM > 1 ? TEAM : kWaves;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (blockIdx.x < P.q_blocks)
-    rope_append_rows<kSrcF32, FS_KV_FP8_BLOCK, HP, false>(P, (int64_t)blockIdx.x * kWaves + wave, (int64_t)P.q_blocks * kWaves);
-  else
-    append_groups<kSrcF32, true, kWaves>(P.a, P.rope, blockIdx.x - P.q_blocks, gridDim.x - P.q_blocks, s_max);
+  const uint32_t cache_blocks = gridDim.x - P.q_blocks;
+  if (SINGLES && blockIdx.x >= cache_blocks) {  // (larger launches rotate the queries in one of their own)
+    rope_append_rows<MODE, kSrcF32, FS_KV_FP8_BLOCK, 1, false>(P, (int64_t)(blockIdx.x - cache_blocks) * kOwn + wave, (int64_t)P.q_blocks * kOwn);
+  } else if constexpr (TEAM == 1) {
+    append_groups<kSrcF32, MODE, 1, LATE, SINGLES>(P.a, P.rope, heads, (int64_t)blockIdx.x * kWaves + wave, (int64_t)cache_blocks * kWaves, nullptr,
+                                                   s_table + wave * table_floats(1));
+  } else {
+    __shared__ float s_max[2 * TEAM];
+    append_groups<kSrcF32, MODE, TEAM, LATE, SINGLES>(P.a, P.rope, heads, blockIdx.x, cache_blocks, s_max, s_table);
+  }
+}
+
+template <int MODE>
+void (*turn_kernel_for(bool src_f32, bool out_f32, bool wide))(TurnArgs) {
+  if (!src_f32) return wide ? turn_kernel<MODE, false, false, kTurnRows> : turn_kernel<MODE, false, false, 1>;
+  if (out_f32) return wide ? turn_kernel<MODE, true, true, kTurnRows> : turn_kernel<MODE, true, true, 1>;
+  return wide ? turn_kernel<MODE, true, false, kTurnRows> : turn_kernel<MODE, true, false, 1>;
+}
+template <int MODE, int DT>
+void (*rope_append_kernel_of(bool f32, bool wide))(RopeAppendArgs) {
+  if (f32) return wide ? rope_append_kernel<MODE, true, DT, kTurnRows> : rope_append_kernel<MODE, true, DT, 1>;
+  return wide ? rope_append_kernel<MODE, false, DT, kTurnRows> : rope_append_kernel<MODE, false, DT, 1>;
+}
+template <int MODE>
+void (*rope_append_kernel_for(int dtype, bool f32, bool wide))(RopeAppendArgs) {
+  switch (dtype) {
+    case FS_KV_FP16: return rope_append_kernel_of<MODE, FS_KV_FP16>(f32, wide);
+    case FS_KV_FP8_E4M3: return rope_append_kernel_of<MODE, FS_KV_FP8_E4M3>(f32, wide);
+    case FS_KV_INT8: return rope_append_kernel_of<MODE, FS_KV_INT8>(f32, wide);
+    default: return rope_append_kernel_of<MODE, FS_KV_INT4>(f32, wide);
+  }
+}
+template <int MODE, bool kF32>
+void (*rope_append_block_kernel_for(const GroupPlan& G))(RopeAppendArgs, int) {
+#define FS_TEAM(TEAM, LATE) (G.singles ? rope_append_block_kernel<MODE, kF32, TEAM, LATE, true> : rope_append_block_kernel<MODE, kF32, TEAM, LATE, false>)
+  return G.late ? FS_TEAM(8, true) : G.team == 8 ? FS_TEAM(8, false) : G.team == 4 ? FS_TEAM(4, false) : FS_TEAM(1, false);
+#undef FS_TEAM
 }
 
 RopeArgs rope_args(const Model& M, int inverse) {
@@ -207,6 +251,24 @@ bool frequencies(const fs_rope_t& r, long double* f) {
     f[i] = x;
   }
   return true;
+}
+
+// Units of `hp` rows of `rows` each token has.
+int64_t row_units(int64_t n_tokens, int lpr_shift, int rows, int hp) {
+  const int64_t tpw = 64 >> lpr_shift;
+  return (n_tokens + tpw - 1) / tpw * ((rows + hp - 1) / hp);
+}
+
+hipError_t launch_turn(const fs_pool* p, const TurnArgs& A, bool src_f32, bool out_f32, hipStream_t s) {
+  const bool wide = row_units(A.n_tokens, A.lpr_shift, A.n_heads, kTurnRows) >= (int64_t)p->n_cu * 32;
+  const int64_t units = row_units(A.n_tokens, A.lpr_shift, A.n_heads, wide ? kTurnRows : 1);
+  const unsigned blocks = (unsigned)std::min<int64_t>((units + kWaves - 1) / kWaves, (int64_t)p->n_cu * 64);
+  const int mode = mode_of(A.rope);
+  void (*const kern)(TurnArgs) = mode == kSplit   ? turn_kernel_for<kSplit>(src_f32, out_f32, wide)
+                                 : mode == kPairs ? turn_kernel_for<kPairs>(src_f32, out_f32, wide)
+                                                  : turn_kernel_for<kMixed>(src_f32, out_f32, wide);
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(kWaves * 64), 0, s, A);
+  return hipGetLastError();
 }
 
 Model* rope_model(fs_pool* p, fs_model_t model, const char* who) {
@@ -294,15 +356,8 @@ extern "C" int fs_rope(fs_pool* p, fs_model_t model, const void* x, int64_t x_st
   A.n_heads = n_heads;
   A.d = d;
   A.lpr_shift = lanes_shift(d);
-  const int64_t tpw = 64 >> A.lpr_shift, groups = (n_tokens + tpw - 1) / tpw;
-  const bool wide = groups * ((n_heads + kTurnRows - 1) / kTurnRows) >= (int64_t)p->n_cu * 32;
-  const int64_t units = groups * (wide ? (n_heads + kTurnRows - 1) / kTurnRows : n_heads);
-  const unsigned blocks = (unsigned)std::min<int64_t>((units + kWaves - 1) / kWaves, (int64_t)p->n_cu * 64);
-  void (*const kern)(TurnArgs) = src_dtype == FS_SRC_FP32 ? (wide ? turn_kernel<true, kTurnRows> : turn_kernel<true, 1>)
-                                                          : (wide ? turn_kernel<false, kTurnRows> : turn_kernel<false, 1>);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(kern, dim3(blocks), dim3(kWaves * 64), 0, (hipStream_t)stream, A);
-  const hipError_t e = hipGetLastError();
+  const hipError_t e = launch_turn(p, A, src_dtype == FS_SRC_FP32, src_dtype == FS_SRC_FP32, (hipStream_t)stream);
   if (e != hipSuccess) return device_error(e, "fs_rope launch");
   return FS_OK;
 }
@@ -353,35 +408,51 @@ extern "C" int fs_rope_append(fs_pool* p, fs_model_t model, int layer, const voi
   P.n_q = n_q_heads;
   P.a.k_stride = k_stride;
   P.a.v_stride = v_stride;
-  const int64_t tpw = 64 >> P.a.lpr_shift, groups = (n_tokens + tpw - 1) / tpw, most = (int64_t)p->n_cu * 64;
-  const bool block = M->g.kv_dtype == FS_KV_FP8_BLOCK;
-  const int rows = n_q_heads + (block ? 0 : 2 * M->g.n_kv_heads);
-  const bool wide = groups * ((rows + kTurnRows - 1) / kTurnRows) >= (int64_t)p->n_cu * 32;
-  const int64_t units = groups * (wide ? (rows + kTurnRows - 1) / kTurnRows : rows);
-  int64_t blocks = std::min((units + kWaves - 1) / kWaves, most);
-  const bool f32 = src_dtype == FS_SRC_FP32;
-  void (*kern)(RopeAppendArgs) = nullptr;
-  if (block) {
-    P.q_blocks = (uint32_t)blocks;
-    P.a.group_chunk = group_chunk(n_tokens, 2 * M->g.n_kv_heads, (int64_t)p->n_cu * 8);
-    blocks += std::min((n_tokens + P.a.group_chunk - 1) / P.a.group_chunk * 2 * M->g.n_kv_heads, most);
-    kern = f32 ? (wide ? rope_append_block_kernel<true, kTurnRows> : rope_append_block_kernel<true, 1>)
-               : (wide ? rope_append_block_kernel<false, kTurnRows> : rope_append_block_kernel<false, 1>);
-  } else {
-#define FS_ROPE_APPEND(DT)                                                                                  \
-  (f32 ? (wide ? rope_append_kernel<true, DT, kTurnRows> : rope_append_kernel<true, DT, 1>)                 \
-       : (wide ? rope_append_kernel<false, DT, kTurnRows> : rope_append_kernel<false, DT, 1>))
-    switch (M->g.kv_dtype) {
-      case FS_KV_FP16: kern = FS_ROPE_APPEND(FS_KV_FP16); break;
-      case FS_KV_FP8_E4M3: kern = FS_ROPE_APPEND(FS_KV_FP8_E4M3); break;
-      case FS_KV_INT8: kern = FS_ROPE_APPEND(FS_KV_INT8); break;
-      default: kern = FS_ROPE_APPEND(FS_KV_INT4); break;
-    }
-#undef FS_ROPE_APPEND
-  }
+  const bool f32 = src_dtype == FS_SRC_FP32, block = M->g.kv_dtype == FS_KV_FP8_BLOCK;
+  hipStream_t const s = (hipStream_t)stream;
   (void)hipGetLastError();
-  hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kWaves * 64), 0, (hipStream_t)stream, P);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipSuccess;
+  const GroupPlan G = block ? plan_groups(p, P.a) : GroupPlan{};
+  // Enough rows for every wave slot: the queries in a launch of their own, whose waves take a third of the registers.
+  if (n_q_heads > 0 && (row_units(n_tokens, P.a.lpr_shift, n_q_heads, kTurnRows) >= (int64_t)p->n_cu * 32 || (block && !G.singles))) {
+    TurnArgs T{};
+    T.rope = P.rope;
+    T.x = q;
+    T.out = q_out;
+    T.pos = pos;
+    T.n_tokens = n_tokens;
+    T.x_stride = q_stride;
+    T.out_stride = q_row;
+    T.n_heads = n_q_heads;
+    T.d = d;
+    T.lpr_shift = P.a.lpr_shift;
+    e = launch_turn(p, T, f32, false, s);
+    if (e != hipSuccess) return device_error(e, "fs_rope_append launch");
+    P.n_q = 0;
+  }
+  const int64_t most = (int64_t)p->n_cu * 64;
+  const int mode = mode_of(P.rope);
+  if (block) {
+    P.a.group_chunk = G.chunk;
+    const int waves = G.team > 1 ? G.team : kWaves;
+    if (P.n_q) P.q_blocks = (uint32_t)std::min((row_units(n_tokens, P.a.lpr_shift, P.n_q, 1) + waves - 1) / waves, most);
+    const size_t lds = (size_t)table_floats(waves) * sizeof(float);  // (8 KB for every wave)
+    void (*const kern)(RopeAppendArgs, int) =
+        mode == kSplit   ? (f32 ? rope_append_block_kernel_for<kSplit, true>(G) : rope_append_block_kernel_for<kSplit, false>(G))
+        : mode == kPairs ? (f32 ? rope_append_block_kernel_for<kPairs, true>(G) : rope_append_block_kernel_for<kPairs, false>(G))
+                         : (f32 ? rope_append_block_kernel_for<kMixed, true>(G) : rope_append_block_kernel_for<kMixed, false>(G));
+    hipLaunchKernelGGL(kern, dim3((unsigned)(G.blocks + P.q_blocks)), dim3(waves * 64), lds, s, P, G.heads);
+  } else {
+    const int rows = P.n_q + 2 * M->g.n_kv_heads;
+    const bool wide = row_units(n_tokens, P.a.lpr_shift, rows, kTurnRows) >= (int64_t)p->n_cu * 32;
+    const int64_t blocks = std::min((row_units(n_tokens, P.a.lpr_shift, rows, wide ? kTurnRows : 1) + kWaves - 1) / kWaves, most);
+    const int dtype = M->g.kv_dtype;
+    void (*const kern)(RopeAppendArgs) = mode == kSplit   ? rope_append_kernel_for<kSplit>(dtype, f32, wide)
+                                         : mode == kPairs ? rope_append_kernel_for<kPairs>(dtype, f32, wide)
+                                                          : rope_append_kernel_for<kMixed>(dtype, f32, wide);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kWaves * 64), 0, s, P);
+  }
+  e = hipGetLastError();
   if (e != hipSuccess) return device_error(e, "fs_rope_append launch");
   return FS_OK;
 }
