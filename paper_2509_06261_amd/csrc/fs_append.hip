@@ -6,17 +6,12 @@
 
 #include "fs_append_block.h"
 
-#ifndef FS_X_HEADS
-#define FS_X_HEADS 4
-#endif
-#ifndef FS_X_TEAMS
-#define FS_X_TEAMS 8
-#endif
 namespace fs {
 namespace {
 
 using namespace append;
 constexpr int kWaves = 4;  // waves per workgroup
+constexpr int kUnitHeads = 4;  // FP8_BLOCK: heads of a unit, at most (see plan_groups)
 
 // The wave's number is made provably uniform, so that a unit's place is found with scalar arithmetic.
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
@@ -106,11 +101,15 @@ append::GroupPlan plan_groups(const fs_pool* p, const append::AppendArgs& A) {
   G.team = A.g.T <= held ? 1 : A.g.T <= 4 * held ? 4 : 8;
   G.late = A.g.T > 8 * held;
   G.singles = A.n_tokens <= 8192;
-  // several heads to a unit where whole blocks of tokens make enough units
+  // Several heads to a unit, which share the group's angles and the search for it, where whole blocks of tokens make enough units.
+  // (us, at most 2 / 4 / 8 heads: 65 600 tokens' keys and values, 8 heads of 128, blocks of 63: 154 / 136 / 141, without a rotation
+  // 82 / 80 / 89; blocks of 128: 219 / 171 / 155 and 123 / 107 / 102; of 16: 149 / 145 / 156; fp32: 196 / 179 / 207.)
   const int64_t groups = std::max<int64_t>(A.n_tokens / A.g.T, 1), full = (int64_t)p->n_cu * 8 / G.team;
-  G.heads = (int)std::min<int64_t>(std::min(H, FS_X_HEADS), std::max<int64_t>(groups * 2 * H / full, 1));
+  G.heads = (int)std::min<int64_t>(std::min(H, kUnitHeads), std::max<int64_t>(groups * 2 * H / full, 1));
   const int parts = 2 * ((H + G.heads - 1) / G.heads);
-  G.chunk = group_chunk(A.n_tokens, parts, (int64_t)p->n_cu * FS_X_TEAMS);
+  // (four units per compute unit and no more: most tokens begin no group.  us, 16 / 8 / 4: one prompt of 777 tokens 21 / 16 / 13, 2100 tokens
+  // of three 21 / 19 / 15, 512 sequences' newest 20 / 16 / 13)
+  G.chunk = group_chunk(A.n_tokens, parts, (int64_t)p->n_cu * 4);
   const int64_t units = (A.n_tokens + G.chunk - 1) / G.chunk * parts;
   G.blocks = std::min(G.team > 1 ? units : (units + kWaves - 1) / kWaves, most);
   return G;

@@ -171,6 +171,20 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
   const bool turned = ROPE != kPlain && which == 0, split = ROPE == rope::kSplit && which == 0;  // (uniform)
   const int64_t t0 = wave * tpw + (lane >> A.lpr_shift);
   const int step = NWV * tpw;
+  int slot[kSteps];
+  rope::Raw<kSrcF32> own[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int64_t t = t0 + (int64_t)s * step;
+    slot[s] = t < G.n ? A.pos[G.first + t] - G.block * g.T : -1;
+  }
+  auto request = [&](int head) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      if (slot[s] >= 0)
+        load_block_row<kSrcF32, ROPE>(src, (G.first + t0 + (int64_t)s * step) * stride + (int64_t)head * g.D, L, which, own[s]);
+  };
+  request(h0);
   int in_table = 0;  // tokens: all that are kept in registers
   if constexpr (ROPE != kPlain) {
     if (turned) {
@@ -185,19 +199,6 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
       }
     }
   }
-  int slot[kSteps];
-  rope::Raw<kSrcF32> own[kSteps];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    const int64_t t = t0 + (int64_t)s * step;
-    slot[s] = t < G.n ? A.pos[G.first + t] - G.block * g.T : -1;
-  }
-  auto request = [&](int head) {
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      if (slot[s] >= 0)
-        load_block_row<kSrcF32, ROPE>(src, (G.first + t0 + (int64_t)s * step) * stride + (int64_t)head * g.D, L, which, own[s]);
-  };
   auto late_row = [&](int head, int64_t t, float (&x)[kEpl]) {  // a row that is not kept
     const int64_t row = (G.first + t) * stride + (int64_t)head * g.D;
     rope::Raw<kSrcF32> w;
@@ -207,7 +208,6 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
       if (turned && L.live) rope::turn_row_at<ROPE, kSrcF32>(R, L, A.pos[G.first + t], x, src, row);
     }
   };
-  request(h0);
   for (int k = 0; k < heads; ++k) {
     const int head = h0 + k;
     const BlockRows B = block_rows(g, G.layer, head, which);

@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kWaves * 64) void rope_append_kernel(RopeAppendArgs
 // FP8_BLOCK: the keys and values by groups of a block's tokens (fs_append_block.h), the queries by rows.  The cache's workgroups
 // come first: they take longest.  TEAM, heads: as in kv_append_block_kernel.  Dynamic LDS: the teams' tables of angles.
 template <int MODE, bool kSrcF32, int TEAM, bool LATE, bool SINGLES>
-__global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64) void rope_append_block_kernel(RopeAppendArgs P, int heads) {
+__global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64, LATE ? 2 : 4) void rope_append_block_kernel(RopeAppendArgs P, int heads) {
   extern __shared__ float s_table[];
   constexpr int kOwn = TEAM > 1 ? TEAM : kWaves;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

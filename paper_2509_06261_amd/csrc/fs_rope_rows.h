@@ -113,11 +113,14 @@ __device__ __forceinline__ Factors<MODE> factors(const RopeArgs& R, const Lane& 
 __device__ __forceinline__ int table_row(const RopeArgs& R) { return ((R.dim >> 1) + 3) & ~3; }
 template <typename Pos>
 __device__ __forceinline__ void fill_table(const RopeArgs& R, float* table, int n_tokens, int thread, int threads, Pos&& pos_of) {
-  const int half = R.dim >> 1, row = table_row(R), n = n_tokens * half;
-#pragma unroll 1
-  for (int i = thread; i < n; i += threads) {
-    const int t = (int)((uint32_t)i / (uint32_t)half), p = i - t * half;
-    angle(R, R.turns[p], pos_of(t), table[t * row + p], table[(n_tokens + t) * row + p]);
+  // a thread keeps to its pair, and as many tokens are worked on side by side as there are threads for
+  const int half = R.dim >> 1, row = table_row(R), wide = min(half, threads), side = threads / wide;
+  const int t0 = thread / wide;
+  if (t0 >= side) return;
+  for (int p = thread - t0 * wide; p < half; p += wide) {
+    const uint64_t turn = R.turns[p];
+#pragma unroll 4
+    for (int t = t0; t < n_tokens; t += side) angle(R, turn, pos_of(t), table[t * row + p], table[(n_tokens + t) * row + p]);
   }
 }
 template <int MODE>
