@@ -176,7 +176,7 @@ class _NotYet:
     def _none(*args):
         return None
 
-    kv_append = kv_append_multi = decode_attention = decode_attention_multi = decode_step_multi = _none
+    kv_append = kv_append_multi = decode_attention = decode_attention_multi = decode_step_multi = rope = rope_append = batch_tables = _none
 
 
 _fast = _NotYet
@@ -191,6 +191,8 @@ def _slow():
                   ("fs_kv_append", "fs_kv_append_multi", "fs_decode_attention", "fs_decode_attention_multi", "fs_decode_step_multi")]
             _fsfast.init(torch.Tensor, torch.float16, torch.float32, torch.int32, ctypes.c_void_p, fs_batch_t, fs_append_t,
                          torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, *at)
+            _fsfast.init_operators(torch.int64, *(ctypes.cast(getattr(_L, f), ctypes.c_void_p).value for f in
+                                                 ("fs_rope", "fs_rope_append", "fs_batch_tables")))
             _fast = _fsfast
 
 
@@ -378,10 +380,13 @@ def _token_stride(x):
 
 def fs_rope(pool, model, x, pos, out, inverse=False, stream=None):
     """x, out: CUDA fp16 or fp32 [n_tokens][n_heads][head_dim], a token's rows contiguous (out may be x); pos: CUDA int32 [n_tokens]."""
-    assert x.dtype == out.dtype and x.dtype in (torch.float16, torch.float32) and x.shape == out.shape
-    assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == x.shape[0]
-    rc = _L.fs_rope(pool, model, _dp(x), _token_stride(x), x.shape[1], FS_SRC_FP32 if x.dtype == torch.float32 else FS_SRC_FP16, _dp(pos),
-                    x.shape[0], int(inverse), _dp(out), _token_stride(out), _stream(stream))
+    rc = _fast.rope(pool, model, x, pos, out, inverse, stream)
+    if rc is None:
+        _slow()
+        assert x.dtype == out.dtype and x.dtype in (torch.float16, torch.float32) and x.shape == out.shape
+        assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == x.shape[0]
+        rc = _L.fs_rope(pool, model, _dp(x), _token_stride(x), x.shape[1], FS_SRC_FP32 if x.dtype == torch.float32 else FS_SRC_FP16, _dp(pos),
+                        x.shape[0], int(inverse), _dp(out), _token_stride(out), _stream(stream))
     if rc != FS_OK:
         raise FsError(rc, "fs_rope")
 
@@ -389,17 +394,20 @@ def fs_rope(pool, model, x, pos, out, inverse=False, stream=None):
 def fs_rope_append(pool, model, layer, q, k, v, seq_idx, pos, block_tables, q_out, stream=None):
     """q: CUDA fp16 or fp32 [n_tokens][n_q_heads][head_dim] (None with q_out None: keys and values alone); k, v: [n_tokens][H][D] of the
     same type, a token's rows contiguous; seq_idx, pos: CUDA int32 [n_tokens]; block_tables: CUDA int32 [n_seq][max_blocks]; q_out: fp16."""
-    assert k.dtype == v.dtype and k.dtype in (torch.float16, torch.float32) and k.shape == v.shape and block_tables.is_contiguous()
-    assert seq_idx.dtype == torch.int32 and pos.dtype == torch.int32 and block_tables.dtype == torch.int32
-    n = seq_idx.numel()
-    assert k.shape[0] == n == pos.numel() and seq_idx.is_contiguous() and pos.is_contiguous() and (q is None) == (q_out is None)
-    n_q = 0
-    if q is not None:
-        assert q.dtype == k.dtype and q.shape == q_out.shape and q.shape[0] == n and q_out.dtype == torch.float16 and q_out.is_contiguous()
-        n_q = q.shape[1]
-    rc = _L.fs_rope_append(pool, model, layer, _dp(q), _token_stride(q) if n_q else 0, n_q, _dp(k), _token_stride(k), _dp(v), _token_stride(v),
-                           FS_SRC_FP32 if k.dtype == torch.float32 else FS_SRC_FP16, _dp(seq_idx), _dp(pos), _dp(block_tables),
-                           block_tables.shape[1], n, _dp(q_out), _stream(stream))
+    rc = _fast.rope_append(pool, model, layer, q, k, v, seq_idx, pos, block_tables, q_out, stream)
+    if rc is None:
+        _slow()
+        assert k.dtype == v.dtype and k.dtype in (torch.float16, torch.float32) and k.shape == v.shape and block_tables.is_contiguous()
+        assert seq_idx.dtype == torch.int32 and pos.dtype == torch.int32 and block_tables.dtype == torch.int32
+        n = seq_idx.numel()
+        assert k.shape[0] == n == pos.numel() and seq_idx.is_contiguous() and pos.is_contiguous() and (q is None) == (q_out is None)
+        n_q = 0
+        if q is not None:
+            assert q.dtype == k.dtype and q.shape == q_out.shape and q.shape[0] == n and q_out.dtype == torch.float16 and q_out.is_contiguous()
+            n_q = q.shape[1]
+        rc = _L.fs_rope_append(pool, model, layer, _dp(q), _token_stride(q) if n_q else 0, n_q, _dp(k), _token_stride(k), _dp(v), _token_stride(v),
+                               FS_SRC_FP32 if k.dtype == torch.float32 else FS_SRC_FP16, _dp(seq_idx), _dp(pos), _dp(block_tables),
+                               block_tables.shape[1], n, _dp(q_out), _stream(stream))
     if rc != FS_OK:
         raise FsError(rc, "fs_rope_append")
 
@@ -408,15 +416,18 @@ def fs_batch_tables(pool, model, held_lens, new_lens, block_ids, block_tables, s
                     stream=None):
     """All CUDA int32 (slots int64, status one element of 32 bits or None): held_lens (or None), new_lens [n_seq]; block_ids [n]; written:
     block_tables [n_seq][max_blocks], seq_lens [n_seq], q_offsets [n_seq + 1], seq_idx, pos, slots (or None) [n_tokens]."""
-    n_seq = new_lens.numel()
-    for t in (held_lens, new_lens, block_ids, block_tables, seq_lens, q_offsets, seq_idx, pos):
-        assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
-    assert block_tables.shape[0] == seq_lens.numel() == n_seq and q_offsets.numel() == n_seq + 1 and pos.numel() == seq_idx.numel()
-    assert held_lens is None or held_lens.numel() == n_seq
-    assert slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == pos.numel())
-    rc = _L.fs_batch_tables(pool, model, _dp(held_lens), _dp(new_lens), n_seq, _dp(block_ids), block_ids.numel(), _dp(block_tables),
-                            block_tables.shape[1], _dp(seq_lens), _dp(q_offsets), _dp(seq_idx), _dp(pos), _dp(slots), pos.numel(), _dp(status),
-                            _stream(stream))
+    rc = _fast.batch_tables(pool, model, held_lens, new_lens, block_ids, block_tables, seq_lens, q_offsets, seq_idx, pos, slots, status, stream)
+    if rc is None:
+        _slow()
+        n_seq = new_lens.numel()
+        for t in (held_lens, new_lens, block_ids, block_tables, seq_lens, q_offsets, seq_idx, pos):
+            assert t is None or (t.dtype == torch.int32 and t.is_contiguous())
+        assert block_tables.shape[0] == seq_lens.numel() == n_seq and q_offsets.numel() == n_seq + 1 and pos.numel() == seq_idx.numel()
+        assert held_lens is None or held_lens.numel() == n_seq
+        assert slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == pos.numel())
+        rc = _L.fs_batch_tables(pool, model, _dp(held_lens), _dp(new_lens), n_seq, _dp(block_ids), block_ids.numel(), _dp(block_tables),
+                                block_tables.shape[1], _dp(seq_lens), _dp(q_offsets), _dp(seq_idx), _dp(pos), _dp(slots), pos.numel(), _dp(status),
+                                _stream(stream))
     if rc != FS_OK:
         raise FsError(rc, "fs_batch_tables")
 

@@ -26,8 +26,15 @@ static struct {
   int (*decode)(fs_pool*, fs_model_t, int, int, float, const void*, const int32_t*, const int32_t*, int, int, void*, float*, void*, uint64_t, void*);
   int (*decode_multi)(fs_pool*, const fs_batch_t*, int, void*, uint64_t, void*);
   int (*decode_step)(fs_pool*, const fs_append_t*, int, const fs_batch_t*, int, void*, uint64_t, void*);
+  /* (init_operators) */
+  int (*rope)(fs_pool*, fs_model_t, const void*, int64_t, int, int, const int32_t*, int64_t, int, void*, int64_t, void*);
+  int (*rope_append)(fs_pool*, fs_model_t, int, const void*, int64_t, int, const void*, int64_t, const void*, int64_t, int, const int32_t*,
+                     const int32_t*, const int32_t*, int, int64_t, void*, void*);
+  int (*tables)(fs_pool*, fs_model_t, const int32_t*, const int32_t*, int, const int32_t*, int64_t, int32_t*, int, int32_t*, int32_t*, int32_t*,
+                int32_t*, int64_t*, int64_t, uint32_t*, void*);
+  PyObject* int64;
 } L;
-static PyObject *s_data_ptr, *s_dtype, *s_is_contiguous, *s_numel, *s_element_size, *s_size, *s_one;
+static PyObject *s_data_ptr, *s_dtype, *s_is_contiguous, *s_numel, *s_element_size, *s_size, *s_one, *s_shape, *s_stride;
 
 /* The helpers below return 1, 0 for "not the fast path's case", or -1 with an exception set. */
 static int is_tensor(PyObject* o) { return (PyObject*)Py_TYPE(o) == L.tensor; }
@@ -127,6 +134,52 @@ static int workspace(PyObject* o, void** out, uint64_t* bytes) {
   if ((ok = method_int(o, s_element_size, &e)) != 1) return ok;
   *bytes = (uint64_t)(n * e);
   return 1;
+}
+
+/* rows [tokens][heads][head_dim] of fp16 or fp32, a token's rows contiguous; stride: elements from token to token (0: one token) */
+typedef struct {
+  int64_t n, heads, d, stride;
+  void* at;
+  int f32;
+} rows_t;
+static int rows_of(PyObject* o, rows_t* r) {
+  PyObject *shape, *step = NULL;
+  int64_t v[6];
+  int i, ok = 0;
+  if (!is_tensor(o)) return 0;
+  if ((r->f32 = has_dtype(o, L.float32, L.float32)) < 0) return -1;
+  if ((i = has_dtype(o, L.float16, L.float32)) != 1) return i;
+  if (!(shape = PyObject_GetAttr(o, s_shape))) return -1;
+  if (PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3) {
+    if (!(step = PyObject_CallMethodNoArgs(o, s_stride))) {
+      Py_DECREF(shape);
+      return -1;
+    }
+    if (PyTuple_Check(step) && PyTuple_GET_SIZE(step) == 3) {
+      ok = 1;
+      for (i = 0; i < 3; ++i) {
+        v[i] = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+        v[3 + i] = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(step, i));
+      }
+    }
+    Py_DECREF(step);
+  }
+  Py_DECREF(shape);
+  if (PyErr_Occurred()) return -1;
+  if (!ok || v[5] != 1 || (v[1] > 1 && v[4] != v[2]) || v[1] > INT_MAX) return 0;
+  r->n = v[0];
+  r->heads = v[1];
+  r->d = v[2];
+  r->stride = v[0] > 1 ? v[3] : 0;
+  return address(o, &r->at);
+}
+static int same_shape(const rows_t* a, const rows_t* b) { return a->n == b->n && a->heads == b->heads && a->d == b->d; }
+/* a contiguous tensor of this type: its address and its elements */
+static int list_of(PyObject* o, PyObject* dtype, void** at, int64_t* n) {
+  int ok;
+  if (!is_tensor(o)) return 0;
+  if ((ok = has_dtype(o, dtype, dtype)) != 1 || (ok = contiguous(o)) != 1 || (ok = method_int(o, s_numel, n)) != 1) return ok;
+  return address(o, at);
 }
 
 #define TRY(x)                       \
@@ -251,6 +304,106 @@ static PyObject* decode_step_multi(PyObject* self, PyObject* const* a, Py_ssize_
   CALL(L.decode_step(pool, ap, ka, b, kb, ws, bytes, stream));
 }
 
+/* (pool, model, x, pos, out, inverse, stream) */
+static PyObject* rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  fs_pool* pool;
+  int model;
+  rows_t x, out;
+  void *pos, *stream;
+  int64_t tokens;
+  (void)self;
+  ARGS(7);
+  if (!L.rope) Py_RETURN_NONE;
+  TRY(bytes_of(a[0], L.c_void_p, &pool, sizeof pool));
+  TRY(plain_int(a[1], &model));
+  TRY(rows_of(a[2], &x));
+  TRY(list_of(a[3], L.int32, &pos, &tokens));
+  TRY(rows_of(a[4], &out));
+  TRY(x.f32 == out.f32 && same_shape(&x, &out) && tokens == x.n && PyBool_Check(a[5]));
+  TRY(stream_of(a[6], &stream));
+  CALL(L.rope(pool, model, x.at, x.stride, (int)x.heads, x.f32 ? FS_SRC_FP32 : FS_SRC_FP16, pos, x.n, a[5] == Py_True, out.at, out.stride, stream));
+}
+
+/* (pool, model, layer, q, k, v, seq_idx, pos, block_tables, q_out, stream) */
+static PyObject* rope_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  fs_pool* pool;
+  int model, layer;
+  rows_t q = {0}, k, v, out = {0};
+  void *seq, *pos, *table, *stream;
+  int64_t tokens, places, entries, blocks;
+  (void)self;
+  ARGS(11);
+  if (!L.rope) Py_RETURN_NONE;
+  TRY(bytes_of(a[0], L.c_void_p, &pool, sizeof pool));
+  TRY(plain_int(a[1], &model));
+  TRY(plain_int(a[2], &layer));
+  TRY(rows_of(a[4], &k));
+  TRY(rows_of(a[5], &v));
+  TRY(list_of(a[6], L.int32, &seq, &tokens));
+  TRY(list_of(a[7], L.int32, &pos, &places));
+  TRY(list_of(a[8], L.int32, &table, &entries));
+  TRY(size1(a[8], &blocks));
+  TRY(k.f32 == v.f32 && same_shape(&k, &v) && k.n == tokens && places == tokens && blocks <= INT_MAX);
+  if (a[3] == Py_None || a[9] == Py_None) {
+    TRY(a[3] == a[9]);
+  } else {
+    TRY(rows_of(a[3], &q));
+    TRY(rows_of(a[9], &out));
+    TRY(contiguous(a[9]));
+    TRY(q.f32 == k.f32 && !out.f32 && same_shape(&q, &out) && q.n == tokens);
+  }
+  TRY(stream_of(a[10], &stream));
+  CALL(L.rope_append(pool, model, layer, q.at, q.stride, (int)q.heads, k.at, k.stride, v.at, v.stride, k.f32 ? FS_SRC_FP32 : FS_SRC_FP16, seq, pos,
+                     table, (int)blocks, tokens, out.at, stream));
+}
+
+/* (pool, model, held_lens, new_lens, block_ids, block_tables, seq_lens, q_offsets, seq_idx, pos, slots, status, stream) */
+static PyObject* batch_tables(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  fs_pool* pool;
+  int model, i;
+  void *p[8] = {0}, *slots = NULL, *status, *stream;
+  int64_t count[8] = {0}, slot_count = 0, blocks;
+  (void)self;
+  ARGS(13);
+  if (!L.rope) Py_RETURN_NONE;
+  TRY(bytes_of(a[0], L.c_void_p, &pool, sizeof pool));
+  TRY(plain_int(a[1], &model));
+  for (i = a[2] == Py_None; i < 8; ++i) TRY(list_of(a[2 + i], L.int32, &p[i], &count[i]));
+  TRY(size1(a[5], &blocks));
+  if (a[10] != Py_None) TRY(list_of(a[10], L.int64, &slots, &slot_count));
+  TRY(address_or_none(a[11], &status));
+  /* new_lens, seq_lens and the table's rows agree, and held_lens if there is one; q_offsets has one more; the token lists agree */
+  TRY((a[2] == Py_None || count[0] == count[1]) && count[4] == count[1] && count[5] == count[1] + 1 && blocks > 0 &&
+      count[3] == count[1] * blocks && count[6] == count[7] && (a[10] == Py_None || slot_count == count[7]) && count[1] <= INT_MAX &&
+      blocks <= INT_MAX);
+  TRY(stream_of(a[12], &stream));
+  CALL(L.tables(pool, model, p[0], p[1], (int)count[1], p[2], count[2], p[3], (int)blocks, p[4], p[5], p[6], p[7], slots, count[7], status, stream));
+}
+
+/* init_operators(int64, addresses of fs_rope, fs_rope_append, fs_batch_tables); init() without arguments forgets them */
+static PyObject* init_operators(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void* fn[3];
+  int i;
+  (void)self;
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "init_operators takes 4 arguments");
+    return NULL;
+  }
+  for (i = 0; i < 3; ++i) {
+    fn[i] = PyLong_AsVoidPtr(a[1 + i]);
+    if (!fn[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null entry point");
+      return NULL;
+    }
+  }
+  Py_INCREF(a[0]);
+  Py_XSETREF(L.int64, a[0]);
+  memcpy(&L.rope, &fn[0], sizeof fn[0]);
+  memcpy(&L.rope_append, &fn[1], sizeof fn[0]);
+  memcpy(&L.tables, &fn[2], sizeof fn[0]);
+  Py_RETURN_NONE;
+}
+
 /* init(Tensor, float16, float32, int32, c_void_p, fs_batch_t, fs_append_t, get_device, get_stream, addresses of the five
  * entry points in the order of L); init() forgets them: every call is answered None until the next one */
 static PyObject* init(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -260,6 +413,8 @@ static PyObject* init(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   (void)self;
   if (n == 0) {
     for (i = 0; i < 9; ++i) Py_CLEAR(*objs[i]);
+    Py_CLEAR(L.int64);
+    L.rope = NULL;
     Py_RETURN_NONE;
   }
   if (n != 14) {
@@ -292,6 +447,10 @@ static PyMethodDef methods[] = {FAST(init, "Types and entry points of the calls.
                                 FAST(decode_attention, "fs_decode_attention, or None."),
                                 FAST(decode_attention_multi, "fs_decode_attention_multi, or None."),
                                 FAST(decode_step_multi, "fs_decode_step_multi, or None."),
+                                FAST(init_operators, "A type and entry points of the calls below."),
+                                FAST(rope, "fs_rope, or None."),
+                                FAST(rope_append, "fs_rope_append, or None."),
+                                FAST(batch_tables, "fs_batch_tables, or None."),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fsfast", "Native marshaling of the binding's device calls.", -1, methods, NULL, NULL, NULL, NULL};
 
@@ -303,6 +462,8 @@ PyMODINIT_FUNC PyInit__fsfast(void) {
   s_element_size = PyUnicode_InternFromString("element_size");
   s_size = PyUnicode_InternFromString("size");
   s_one = PyLong_FromLong(1);
-  if (!s_data_ptr || !s_dtype || !s_is_contiguous || !s_numel || !s_element_size || !s_size || !s_one) return NULL;
+  s_shape = PyUnicode_InternFromString("shape");
+  s_stride = PyUnicode_InternFromString("stride");
+  if (!s_shape || !s_stride || !s_data_ptr || !s_dtype || !s_is_contiguous || !s_numel || !s_element_size || !s_size || !s_one) return NULL;
   return PyModule_Create(&module);
 }
