@@ -20,8 +20,8 @@
 //   The head dimension decides the counts only: HD / 32 k-steps for S^T, HD / 16 output columns per lane (one
 //   16x16 accumulator tile each), HD / 16 elements of every V row per lane.
 //
-// Dequantization is folded around the MFMAs (FP8_BLOCK's scales into the conversion of the codes): FP8 static scales and INT8/INT4 per-token K scales
-// multiply the logits, per-token V scales multiply P; integer codes enter the MFMA unconverted, as fp16
+// Dequantization is folded around the MFMAs: FP8 static scales, FP8_BLOCK's K scales and INT8/INT4 per-token K scales
+// multiply the logits, per-token V scales multiply P, FP8_BLOCK's V scales go into the conversion of the codes; integer codes enter the MFMA unconverted, as fp16
 // subnormals, and their offsets (128 for INT8, the zero-point for INT4) come back as rank-1
 // corrections (z_k * sum(q) on the logits, sum_t p_t s_t z_t on the output).
 #pragma once
@@ -37,6 +37,7 @@ namespace {
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -161,16 +162,15 @@ constexpr float kNoReference = -3.402823466e38f;
 
 // GP = padded group size: 4 when the KV head serves at most 4 query heads, else 16.  The MFMAs always work on 16
 // head columns; GP decides how the softmax between them is spread over the lanes (see softmax_pv).
-// FP8_BLOCK adds the scales of the K rows and of the V rows that the lane holds (a run lies in one block).
+// FP8_BLOCK adds the scales of the lane's run j of V rows (a run lies in one block).  They come with one load: the logits that the lane
+// gets out of S^T are those of run j too, so K's scale multiplies them there, and V's goes into the conversion of the codes.
 template <int DT>
 struct TileScales {
-  __device__ __forceinline__ float k_scale() const { return 1.0f; }
   __device__ __forceinline__ float v_scale() const { return 1.0f; }
 };
 template <>
 struct TileScales<FS_KV_FP8_BLOCK> {
   float ks, vs;
-  __device__ __forceinline__ float k_scale() const { return ks; }
   __device__ __forceinline__ float v_scale() const { return vs; }
 };
 template <int DT, int GP, int HD = 128>
@@ -211,7 +211,6 @@ __device__ __forceinline__ void issue_k(const ItemCtx& X, int vb, int j, int c, 
   // row m = c of S^T tile u is slot 4u + (c & 3) of run c >> 2
   const RunLoc L = locate(X, vb, c >> 2);
   const gptr p = L.base + (uint32_t)((L.start + (c & 3)) * F::kRowBytes) + F::kKLane * j;
-  if constexpr (DT == FS_KV_FP8_BLOCK) t.ks = *reinterpret_cast<const FS_GLOBAL float*>(L.base + X.scale_off);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -293,7 +292,11 @@ template <int DT, int GP, int HD, bool WIDE = false, bool STREAM = false>
 __device__ __forceinline__ void issue_v(const ItemCtx& X, const DevGeom& g, int vb, int j, int c, Tile<DT, GP, HD>& t) {
   using F = Fmt<DT, HD>;
   const RunLoc L = locate(X, vb, j);
-  if constexpr (DT == FS_KV_FP8_BLOCK) t.vs = *reinterpret_cast<const FS_GLOBAL float*>(L.base + X.scale_off + 4);
+  if constexpr (DT == FS_KV_FP8_BLOCK) {
+    const float2v both = *reinterpret_cast<const FS_GLOBAL float2v*>(L.base + X.scale_off);
+    t.ks = both[0];
+    t.vs = both[1];
+  }
   if constexpr (F::kParBytes != 0) {  // parameters first: the softmax needs them before the V rows
     const gptr pk = L.base + 2u * g.kv_tile;
     if constexpr (GP == 16) {
@@ -528,7 +531,7 @@ __device__ __forceinline__ void qk_tile(const Tile<DT, GP, HD>& t, const u32x4 (
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     u32x4 a[HD / 32];
-    k_operands<DT, HD>(t.k[u], a, t.k_scale());
+    k_operands<DT, HD>(t.k[u], a);
     float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < HD / 32; ++ks) acc = mfma(a[ks], qb[ks], acc);
@@ -592,6 +595,7 @@ template <int DT, int GP, int HD, bool DECODE>
 __device__ __forceinline__ void softmax_pv(const ItemCtx& X, Tile<DT, GP, HD>& t, const float4v (&s)[2], int vb, int j, int c,
                                            float qsum, float alpha, StateT<HD>& st) {
   using F = Fmt<DT, HD>;
+  if constexpr (DT == FS_KV_FP8_BLOCK) alpha *= t.ks;
   const RunGeom L = run_geom(X, vb + j);
   const bool partial = !__all(L.lo == 0 && L.hi == 8);  // wave-uniform
   const uint32_t n_ok = (uint32_t)max(L.hi - L.lo, 0);  // of a partial tile: slot i of the run is live iff (unsigned)(i - lo) < n_ok

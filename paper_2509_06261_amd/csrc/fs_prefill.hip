@@ -1296,7 +1296,6 @@ __device__ __forceinline__ uint32_t count_piece(const PrefillArgs& P, uint32_t a
 // A pair of a piece's numbers, written to and read from where every XCD sees it (agent scope: past the XCDs' own L2s).  us, with a
 // write-back of the L2 by every wave in front of the count -> like this: four FP8 chunks of 512 behind 3000 - 16384 379 -> 302, 300
 // FP16 ones of 16 behind 200 - 4000 with one KV head 293 -> 126, 14 of 100 with 40 heads 441 -> 244.
-typedef float float2v __attribute__((ext_vector_type(2)));
 typedef unsigned long long Pair;
 __device__ __forceinline__ void leave_pair(Pair* at, float x, float y) {
   __hip_atomic_store(at, (Pair)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
