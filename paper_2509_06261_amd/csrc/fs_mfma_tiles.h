@@ -171,6 +171,7 @@ struct TileScales {
 template <>
 struct TileScales<FS_KV_FP8_BLOCK> {
   float ks, vs;
+  int vk;  // (workgroup prefill, whose scales lie in LDS: the block that this lane takes a V row's scale of)
   __device__ __forceinline__ float v_scale() const { return vs; }
 };
 template <int DT, int GP, int HD = 128>

@@ -656,21 +656,23 @@ constexpr uint32_t stage_v(int subs, int hd = kD) { return (uint32_t)(subs * fra
 constexpr uint32_t stage_par(int subs, int hd = kD) { return 2 * stage_v(subs, hd); }
 constexpr uint32_t stage_bytes(int subs, int hd = kD) { return stage_par(subs, hd) + (uint32_t)subs * 256; }
 constexpr uint32_t kWgCtlBytes = 16;
+// the table of a segment's blocks: addresses, and behind them FP8_BLOCK's scales of the item's head
+constexpr uint32_t table_entry_bytes(int kv_dtype) { return kv_dtype == FS_KV_FP8_BLOCK ? 16 : 8; }
 
 template <int DT, int HD>
-__device__ __forceinline__ void stage_k(uint8_t* stage, int sub, int lane, Tile<DT, 16, HD>& t, const uint32_t (&kpar)[2]) {  // (K fragments lead the stage)
+__device__ __forceinline__ void stage_k(uint8_t* stage, int sub, int lane, Tile<DT, 16, HD>& t, const uint32_t (&kpar)[2], const float2v* scales) {  // (K fragments lead the stage)
   constexpr int KS = HD / 32;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     u32x4 a[KS];
-    k_operands<DT, HD>(t.k[u], a, DT == FS_KV_FP8_BLOCK ? __uint_as_float(kpar[u]) : 1.0f);
+    k_operands<DT, HD>(t.k[u], a, DT == FS_KV_FP8_BLOCK ? scales[kpar[u]][0] : 1.0f);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
       *reinterpret_cast<u32x4*>(stage + (uint32_t)(((sub * 2 + u) * KS + ks) * kFrag) + lane * 16) = a[ks];
   }
 }
 template <int DT, int SUBS, int HD>
-__device__ __forceinline__ void stage_v(uint8_t* stage, int sub, int lane, bool clear, int live, Tile<DT, 16, HD>& t) {
+__device__ __forceinline__ void stage_v(uint8_t* stage, int sub, int lane, bool clear, int live, Tile<DT, 16, HD>& t, const float2v* scales) {
   using F = Fmt<DT, HD>;
   if constexpr (DT == FS_KV_FP16 || e4m3_codes<DT>()) {
     // slots past the sequence's end may hold NaN/Inf bit patterns; 0 * NaN would poison the MFMA
@@ -682,8 +684,9 @@ __device__ __forceinline__ void stage_v(uint8_t* stage, int sub, int lane, bool 
     }
   }
   uint32_t vx[8][F::kVRegs];
-  if constexpr (DT == FS_KV_FP8_BLOCK) {  // (slot i's scale: fetched by lane i of the row)
-    static_for(std::make_integer_sequence<int, 8>{}, [&](auto I) { v_unpack<DT, HD>(t.v[decltype(I)::value], vx[decltype(I)::value], row_bcast<decltype(I)::value>(t.vs)); });
+  if constexpr (DT == FS_KV_FP8_BLOCK) {  // (slot i's scale: lane i of the row has it)
+    const float vs = scales[t.vk][1];
+    static_for(std::make_integer_sequence<int, 8>{}, [&](auto I) { v_unpack<DT, HD>(t.v[decltype(I)::value], vx[decltype(I)::value], row_bcast<decltype(I)::value>(vs)); });
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v_unpack<DT, HD>(t.v[i], vx[i]);
@@ -770,7 +773,7 @@ __device__ __forceinline__ void dequant8(const uint32_t* w, const Deq<DT>& q, ui
 struct TokenCtx {
   const uint64_t* ptr;  // LDS: addresses of the blocks' layers from the segment's first block on
   uint64_t base_off;    // of the KV head
-  uint64_t scale_off;   // FP8_BLOCK: from the head's chunk to its scales
+  const float2v* scales;  // LDS, FP8_BLOCK: the head's scales of K and V in those blocks
   int rel0;             // the segment's first token within its first block
   int last;             // the segment's last token, counted from its first one
   int T;
@@ -790,7 +793,7 @@ __device__ __forceinline__ TokenPlace place_token(const TokenCtx& X, int t) {
 }
 
 // K rows of the sub-tile from token tb of the segment on: row c of half-tile u is token 8 (c / 4) + 4 u + c % 4.
-// kpar (PAR): their parameters
+// kpar (PAR): their parameters (FP8_BLOCK: the blocks they are in)
 template <int DT, int HD, bool PAR>
 __device__ __forceinline__ void fetch_k(const TokenCtx& X, const DevGeom& g, bool whole, int tb, int j, int c, Tile<DT, 16, HD>& t,
                                         uint32_t (&kpar)[2]) {
@@ -801,7 +804,7 @@ __device__ __forceinline__ void fetch_k(const TokenCtx& X, const DevGeom& g, boo
 #pragma unroll
     for (int s = 0; s < F::kKLoads; ++s) t.k[u][s] = *reinterpret_cast<const FS_GLOBAL kvec*>(at + 4 * F::kKLane * s);
     if constexpr (DT == FS_KV_FP8_BLOCK) {
-      kpar[u] = *reinterpret_cast<const FS_GLOBAL uint32_t*>(p.base + X.scale_off);
+      kpar[u] = (uint32_t)p.k;
     } else if constexpr (PAR) {
       const gptr pp = p.base + 2u * g.kv_tile + (uint32_t)(p.slot * F::kParBytes);
       if constexpr (F::kParBytes == 2) kpar[u] = *reinterpret_cast<const FS_GLOBAL uint16_t*>(pp);
@@ -829,10 +832,7 @@ __device__ __forceinline__ void fetch_v(const TokenCtx& X, const DevGeom& g, boo
   const int run = tb + 8 * j;
   const RunRows R = run_rows(X.rel0, X.last, X.T, X.magic, run, whole);
   const TokenPlace p{(gptr)(X.ptr[R.k] + X.base_off), R.k, R.slot};
-  if constexpr (DT == FS_KV_FP8_BLOCK) {  // lane c: the scale of token c % 8's block
-    const gptr base = whole ? p.base : place_token(X, min(run + (c & 7), X.last)).base;
-    t.vs = *reinterpret_cast<const FS_GLOBAL float*>(base + X.scale_off + 4);
-  }
+  if constexpr (DT == FS_KV_FP8_BLOCK) t.vk = whole ? p.k : place_token(X, min(run + (c & 7), X.last)).k;  // (of token c % 8)
   if constexpr (F::kParBytes != 0) {  // parameters first: they are needed before the rows
     TokenPlace o = p;
     if (whole) o.slot += c & 7;
@@ -1427,9 +1427,10 @@ __device__ void prefill_item_wg(const PrefillArgs& P, uint32_t* header, int seq,
   TokenCtx X;
   X.ptr = s_tab;
   X.base_off = (uint64_t)head * g.head_chunk;
-  X.scale_off = DT == FS_KV_FP8_BLOCK ? scale_offset(g, head) : 0;
   X.T = g.T;
   X.magic = P.t_magic;
+  float2v* const s_scale = reinterpret_cast<float2v*>(s_tab + P.table_entries);
+  X.scales = s_scale;
 
   u32x4 qb[NCB][HD / 32];
   int len_cb[NCB], row_cb[NCB];
@@ -1490,11 +1491,19 @@ __device__ void prefill_item_wg(const PrefillArgs& P, uint32_t* header, int seq,
         if (does_k) stage_k_int<DT, HD>(stage, sw, lane, t, kpar);
         if (does_v) stage_v_int<DT, SUBS, HD>(stage, sw, lane, clear, live, alpha, t);
       } else {
-        if (does_k) stage_k<DT, HD>(stage, sw, lane, t, kpar);
-        if (does_v) stage_v<DT, SUBS, HD>(stage, sw, lane, clear, live, t);
+        if (does_k) stage_k<DT, HD>(stage, sw, lane, t, kpar, X.scales);
+        if (does_v) stage_v<DT, SUBS, HD>(stage, sw, lane, clear, live, t, X.scales);
       }
     };
     fetch(32 * sw);
+    if constexpr (DT == FS_KV_FP8_BLOCK) {
+      // The segment's scales of this head go to LDS once (after the last readers' barrier, as the table): fetched with every sub-tile
+      // they were one more line to wait for in each step.  us: 64 chunks of 4 tokens behind 6000 303 -> 245, 100 of 16 behind 4000 348 ->
+      // 289; 64 prompts of 4096 8260 -> 8040.
+      const uint64_t off = X.base_off + scale_offset(g, head);
+      for (int i = threadIdx.x; i <= (X.rel0 + n - 1) / g.T; i += NW * 64) s_scale[i] = *reinterpret_cast<const FS_GLOBAL float2v*>((gptr)(s_tab[i] + off));
+      __syncthreads();
+    }
     stage_to(smem, 32 * sw);
     __syncthreads();
 #ifdef FS_TIMELINE
@@ -1748,10 +1757,10 @@ __device__ void prefill_item_wgp(const PrefillArgs& P, int seq, int head, int qt
     issue_k<DT, 16>(X, v0 + 4 * w, j, c, t);
     issue_v<DT, 16>(X, g, v0 + 4 * w, j, c, t);
     const uint32_t no_par[2] = {0u, 0u};
-    stage_k<DT, kD>(smem, w, lane, t, no_par);
+    stage_k<DT, kD>(smem, w, lane, t, no_par, nullptr);
     {
       const int live = locate(X, v0 + 4 * w, j).hi_u;
-      stage_v<DT, SUBS, kD>(smem, w, lane, !__all(live >= 8), live, t);
+      stage_v<DT, SUBS, kD>(smem, w, lane, !__all(live >= 8), live, t, nullptr);
     }
     __syncthreads();
 #pragma unroll
@@ -1863,10 +1872,10 @@ __device__ void prefill_item_wgp(const PrefillArgs& P, int seq, int head, int qt
         }
       }
       uint8_t* next = smem + (uint32_t)((i + 1) & 1) * stage_bytes(SUBS);
-      stage_k<DT, kD>(next, w, lane, t, no_par);
+      stage_k<DT, kD>(next, w, lane, t, no_par, nullptr);
       {
         const int live = locate(X, vb_next, j).hi_u;
-        stage_v<DT, SUBS, kD>(next, w, lane, !__all(live >= 8), live, t);
+        stage_v<DT, SUBS, kD>(next, w, lane, !__all(live >= 8), live, t, nullptr);
       }
       __syncthreads();
     }
@@ -2263,11 +2272,12 @@ __device__ __forceinline__ void prefill_groups(const PrefillArgs& P) {
   const DevBatch& B = P.b;
   uint8_t* smem = reinterpret_cast<uint8_t*>(smem64);
   uint64_t* s_tab = reinterpret_cast<uint64_t*>(smem + 2 * stage_bytes(SUBS, HD));
-  uint32_t* s_ctl = reinterpret_cast<uint32_t*>(smem + 2 * stage_bytes(SUBS, HD) + (size_t)P.table_entries * 8);
+  constexpr uint32_t kEntry = table_entry_bytes(DT);
+  uint32_t* s_ctl = reinterpret_cast<uint32_t*>(smem + 2 * stage_bytes(SUBS, HD) + (size_t)P.table_entries * kEntry);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t H = (uint32_t)B.g.H;
-  uint32_t* s_tf = reinterpret_cast<uint32_t*>(smem + 2 * stage_bytes(SUBS, HD) + (size_t)P.table_entries * 8 + kWgCtlBytes);
+  uint32_t* s_tf = reinterpret_cast<uint32_t*>(smem + 2 * stage_bytes(SUBS, HD) + (size_t)P.table_entries * kEntry + kWgCtlBytes);
   const bool direct = GROUPS || SPLIT || (!PIPE && P.direct);  // (uniform)
   uint32_t* const header = direct ? P.header + kHdrIgnored - kHdrStatus : P.header;
   const uint32_t* tf = P.tile_first;
@@ -2683,7 +2693,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
                workspace_bytes >= fs_prefill_workspace_bytes(n_seq);
   P.plan_items = (int32_t)((items + 7) / 8 * 8);
   P.pieces = (uint8_t*)workspace + pieces_at(n_seq);
-  const size_t smem_split = 2 * (size_t)stage_bytes(4, g.head_dim) + (size_t)P.table_entries * 8 + kWgCtlBytes + seq_list_bytes(n_seq) +
+  const size_t smem_split = 2 * (size_t)stage_bytes(4, g.head_dim) + (size_t)P.table_entries * table_entry_bytes(g.kv_dtype) + kWgCtlBytes + seq_list_bytes(n_seq) +
                             split_plan_bytes((uint32_t)P.plan_items);
   if (smem_split > 160 * 1024) split = false;
   if (split) P.direct = 1;
@@ -2733,7 +2743,7 @@ int fs_prefill_attention(fs_pool* p, fs_model_t model, int layer, int n_q_heads,
   // 105 -> 110 (all three in the queue, behind a preparation launch: 192, 155, 86 and 142).
   P.by_tile = wg && (split || g.n_kv_heads % 8 == 0 || g.n_kv_heads == 4 || (g.n_kv_heads <= 2 && items <= 20 * (uint64_t)p->n_cu));
   if (P.by_tile) P.chunk_shift = 0;
-  const size_t smem = split ? smem_split : wg ? 2 * (size_t)stage_bytes(subs, g.head_dim) + (size_t)P.table_entries * 8 + kWgCtlBytes +
+  const size_t smem = split ? smem_split : wg ? 2 * (size_t)stage_bytes(subs, g.head_dim) + (size_t)P.table_entries * table_entry_bytes(g.kv_dtype) + kWgCtlBytes +
                                (P.tf_cache == 2 ? seq_list_bytes(n_seq) : P.tf_cache ? (((size_t)n_seq + 1) * 4 + 15) / 16 * 16 : 0)
                          : (size_t)kWaves * P.table_entries * sizeof(uint64_t);
   if (wg) {
