@@ -340,7 +340,7 @@ extern "C" int fs_rope(fs_pool* p, fs_model_t model, const void* x, int64_t x_st
     set_error("fs_rope: rows must not overlap and must be 16-byte aligned");
     return FS_ERR_INVALID;
   }
-  if (!M->d_turns) {
+  if (M->rope_dim == 0) {
     set_error("fs_rope: the model has no rotation (fs_model_set_rope)");
     return FS_ERR_INVALID;
   }
@@ -396,7 +396,7 @@ extern "C" int fs_rope_append(fs_pool* p, fs_model_t model, int layer, const voi
   RopeAppendArgs P{};
   const int rc = make_append_args(p, a, P.a);
   if (rc != FS_OK) return rc;
-  if (!M->d_turns) {
+  if (M->rope_dim == 0) {
     set_error("fs_rope_append: the model has no rotation (fs_model_set_rope)");
     return FS_ERR_INVALID;
   }

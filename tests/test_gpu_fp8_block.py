@@ -470,6 +470,16 @@ def test_prefill(heads, group, d, t, lens, new):
     c.close()
 
 
+@pytest.mark.parametrize("heads,group,d,t,lens,new", [
+    (2, 4, 128, 5, [5000, 2500, 2432], [100, 60, 1]), (1, 8, 64, 8, [9000, 8193], [300, 2]), (2, 4, 256, 3, [3300, 1409], [40, 9]), (8, 4, 128, 16, [9000, 8192], [400, 300]),
+    (8, 4, 128, 7, [3700] * 9, [260] * 9)])
+def test_prefill_of_more_blocks_than_a_table_holds(heads, group, d, t, lens, new):
+    c = Cache(heads, d, t, lens)
+    out, lse, q, off = prefill(c, group, 0.07, new)
+    compare(c, out, lse, q, group, 0.07, some_rows(c, off, new, c.rng, most=10))
+    c.close()
+
+
 def compare_out_only(c, out, q, group, scale, rows):
     out = out.double().cpu().numpy()
     for r, i, n in rows:

@@ -243,3 +243,73 @@ def test_padding_and_tokens_without_a_block(kind):
     assert torch.equal(c.mem, before)
     fs.fs_rope_append(c.pool, c.model, 0, q[:0], k[:0], v[:0], seq[:0], pos[:0], c.table, q_out[:0])
     c.close()
+
+
+def both_appends(kind, src, heads, group, d, t, rope, lens, pads, seed):
+    """One call, and fs_rope with fs_kv_append: the same bytes and the same queries.  Returns q, q_out, positions."""
+    import torch
+    lens = np.array(lens)
+    a, b = (Cache(kind, heads, d, t, 2, lens, 7, rope) for _ in range(2))
+    rng = np.random.default_rng(seed)
+    dt = torch.float16 if src == "fp16" else torch.float32
+    held = np.zeros_like(lens)
+    for upto in (np.maximum(lens // 40, 1), lens):  # few tokens, then the many
+        seq, pos = new_tokens(upto, held)
+        held = upto
+        if pads:  # behind every sequence a few tokens of nobody
+            cuts = np.cumsum(np.unique(seq, return_counts=True)[1])
+            seq, pos = (np.insert(x, np.repeat(cuts, pads), f) for x, f in ((seq, 0), (pos, -1)))
+        seq, pos = torch.from_numpy(seq).cuda(), torch.from_numpy(pos).cuda()
+        n, nq = len(seq), heads * group
+        qkv = (torch.randn((n, (nq + 2 * heads) * d), device="cuda", generator=torch.Generator("cuda").manual_seed(seed)) * 2).to(dt)
+        q, k, v = (x.view(n, -1, d) for x in qkv.split([nq * d, heads * d, heads * d], dim=1))
+        q_out, q_ref = (torch.full((n, nq, d), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+        fs.fs_rope_append(a.pool, a.model, 1, q, k, v, seq, pos, a.table, q_out)
+        k32, q32 = torch.zeros((n, heads, d), device="cuda"), torch.zeros((n, nq, d), device="cuda")
+        fs.fs_rope(b.pool, b.model, k.float().contiguous(), pos, k32)
+        fs.fs_kv_append(b.pool, b.model, 1, k32, v.float().contiguous(), seq, pos, b.table)
+        fs.fs_rope(b.pool, b.model, q.float().contiguous(), pos, q32)
+        q_ref[pos >= 0] = q32[pos >= 0].half()
+        assert torch.equal(a.mem, b.mem)
+        assert torch.equal(q_out, q_ref)
+    a.close()
+    b.close()
+    return q, q_out, pos
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("src", ["fp16", "fp32"])
+@pytest.mark.parametrize("r,halves", [(64, True), (64, False), (42, True)])
+def test_prompts_of_many_tokens(kind, src, r, halves):
+    """More rows than the card has waves: the queries go by themselves, and FP8_BLOCK's groups are cut differently."""
+    q, q_out, pos = both_appends(kind, src, 8, 4, 64, 17, fs.make_rope(r, 10000.0, layout=int(not halves)), [5000, 4400, 1, 16, 18], 3, 2)
+    some = np.random.default_rng(1).permutation(np.flatnonzero(pos.cpu().numpy() >= 0))[:50]
+    check_rotated(q_out[some].double().cpu().numpy(), q[some].double().cpu().numpy(), pos.cpu().numpy()[some], plain.frequencies(r, 10000.0, "none"), halves, "fp16", from_fp32=src == "fp32")
+
+
+@pytest.mark.parametrize("src", ["fp16", "fp32"])
+@pytest.mark.parametrize("heads,group,d,t,r,halves,lens", [
+    (2, 2, 256, 100, 256, True, [200, 199, 5]), (3, 1, 128, 200, 128, False, [1000, 201]), (1, 8, 512, 70, 100, True, [140, 3]), (2, 1, 64, 400, 22, True, [900, 400, 401]),
+    (1, 1, 128, 200, 128, True, [9000, 100])])
+def test_blocks_of_more_rows_than_fit_in_registers(src, heads, group, d, t, r, halves, lens):
+    both_appends("block", src, heads, group, d, t, fs.make_rope(r, 10000.0, layout=int(not halves)), lens, 0, 4)
+
+
+def test_rotation_of_many_rows():
+    """The launches whose waves take several rows: against the definition at rows drawn over all of them."""
+    import torch
+    rng = np.random.default_rng(6)
+    for d, r, halves in ((128, 128, True), (64, 64, False), (128, 126, True)):
+        pool, m, mem = make_model(d)
+        fs.fs_model_set_rope(pool, m, fs.make_rope(r, 10000.0, layout=int(not halves)))
+        for dt in (torch.float16, torch.float32):
+            x = torch.randn((9001, 33, d), device="cuda").to(dt)
+            pos = torch.from_numpy(rng.integers(0, 100000, 9001).astype(np.int32)).cuda()
+            pos[77] = -1
+            out = torch.full_like(x, 3.0)
+            fs.fs_rope(pool, m, x, pos, out)
+            assert (out[77] == 3).all()
+            some = rng.permutation(9001)[:60]
+            some = np.concatenate([some[some != 77], [0, 1, 8999, 9000]])
+            check_rotated(out[some].double().cpu().numpy(), x[some].double().cpu().numpy(), pos.cpu().numpy()[some], plain.frequencies(r, 10000.0, "none"), halves, "fp16" if dt == torch.float16 else "fp32")
+        fs.fs_pool_destroy(pool)
