@@ -221,7 +221,7 @@ int fs_rope_frequencies(const fs_rope_t* rope, double* radians);
 int fs_rope(fs_pool* pool, fs_model_t model, const void* x, int64_t x_stride, int n_heads, int src_dtype, const int32_t* pos,
             int64_t n_tokens, int inverse, void* out, int64_t out_stride, void* stream);
 
-/* The new tokens of one layer between the projections and the attention call, in one launch: queries are rotated into q_out,
+/* The new tokens of one layer between the projections and the attention call, in one call: queries are rotated into q_out,
  * keys are rotated and appended, values appended.  Same as fs_rope on the queries and fs_kv_append of the rotated fp32 keys (the
  * keys are rounded once, to the cache's format).
  *   q, k, v : device, [n_tokens] rows of n_q_heads (n_kv_heads) x head_dim of src_dtype; the strides are elements from a token's
@@ -248,7 +248,7 @@ int fs_rope_append(fs_pool* pool, fs_model_t model, int layer, const void* q, in
  *   slots[i] (or NULL) = Blk ID * T + slot in the block, the token's row in the pool; behind the last new token -1 in all three
  *   (calls with a fixed number of tokens skip those), and -1 in slots where the token's block is none of the pool
  *   status (or NULL): 0, or a bit mask -- 1: a length was negative or beyond max_blocks * T (clamped into 0 .. that); 2: block_ids or
- *   the token lists were too short.  Tokens that find no place in the lists are cut: they count in neither seq_lens nor q_offsets.
+ *   the token lists were too short.  Tokens that find no place in the token lists are cut: they count in neither seq_lens nor q_offsets.
  * All device int32 (slots int64, status uint32); no two of the written arrays, and none of them and a read one, may overlap.
  * block_tables' entries for the held tokens are read where slots is asked for. */
 int fs_batch_tables(fs_pool* pool, fs_model_t model, const int32_t* held_lens, const int32_t* new_lens, int n_seq,

@@ -22,13 +22,13 @@ __global__ __launch_bounds__(kWaves * 64) void kv_append_kernel(AppendArgs A) {
 }
 
 // FP8_BLOCK models.  TEAM: waves that work on a group together.
-template <bool kSrcF32, int TEAM, bool LATE, bool SINGLES>
+template <bool kSrcF32, int TEAM, bool LATE>
 __global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64) void kv_append_block_kernel(AppendArgs A, int heads) {
   if constexpr (TEAM == 1) {
-    append_groups<kSrcF32, kPlain, 1, LATE, SINGLES>(A, rope::RopeArgs{}, heads, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves, nullptr, nullptr);
+    append_groups<kSrcF32, kPlain, 1, LATE>(A, rope::RopeArgs{}, heads, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves, nullptr, nullptr);
   } else {
     __shared__ float s_max[2 * TEAM];
-    append_groups<kSrcF32, kPlain, TEAM, LATE, SINGLES>(A, rope::RopeArgs{}, heads, blockIdx.x, gridDim.x, s_max, nullptr);
+    append_groups<kSrcF32, kPlain, TEAM, LATE>(A, rope::RopeArgs{}, heads, blockIdx.x, gridDim.x, s_max, nullptr);
   }
 }
 
@@ -100,7 +100,6 @@ append::GroupPlan plan_groups(const fs_pool* p, const append::AppendArgs& A) {
   const int held = (64 >> A.lpr_shift) * append::kSteps;  // rows that a wave keeps
   G.team = A.g.T <= held ? 1 : A.g.T <= 4 * held ? 4 : 8;
   G.late = A.g.T > 8 * held;
-  G.singles = A.n_tokens <= 8192;
   // Several heads to a unit, which share the group's angles and the search for it, where whole blocks of tokens make enough units.
   // (us, at most 2 / 4 / 8 heads: 65 600 tokens' keys and values, 8 heads of 128, blocks of 63: 154 / 136 / 141, without a rotation
   // 82 / 80 / 89; blocks of 128: 219 / 171 / 155 and 123 / 107 / 102; of 16: 149 / 145 / 156; fp32: 196 / 179 / 207.)
@@ -162,9 +161,7 @@ extern "C" int fs_kv_append(fs_pool* p, fs_model_t model, int layer, const void*
     const append::GroupPlan G = plan_groups(p, A);
     A.group_chunk = G.chunk;
     void (*kern)(AppendArgs, int) = nullptr;
-#define FS_APPEND(TEAM, LATE)                                                                                                   \
-  (G.singles ? (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE, true> : kv_append_block_kernel<false, TEAM, LATE, true>)   \
-             : (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE, false> : kv_append_block_kernel<false, TEAM, LATE, false>))
+#define FS_APPEND(TEAM, LATE) (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE> : kv_append_block_kernel<false, TEAM, LATE>)
     kern = G.late ? FS_APPEND(8, true) : G.team == 8 ? FS_APPEND(8, false) : G.team == 4 ? FS_APPEND(4, false) : FS_APPEND(1, false);
 #undef FS_APPEND
     (void)hipGetLastError();

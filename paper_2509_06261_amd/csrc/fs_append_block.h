@@ -322,9 +322,9 @@ __device__ __forceinline__ void append_singles(const AppendArgs& A, const rope::
 }
 
 // One append, dealt to n_teams teams of NWV waves; this one is number `team`.  A unit: the groups that begin among
-// A.group_chunk neighbouring tokens, of them `heads` heads' K or V rows.
-// SINGLES: groups of one token apart from the others.
-template <bool kSrcF32, int ROPE, int NWV, bool LATE, bool SINGLES>
+// A.group_chunk neighbouring tokens, of them `heads` heads' K or V rows.  Groups of one token, a decode step's, are worked on side by side
+// (16 384 of them 55 us; as groups like the others, one after the other, 385; prompts take the same with either, 125 and 123).
+template <bool kSrcF32, int ROPE, int NWV, bool LATE>
 __device__ __forceinline__ void append_groups(const AppendArgs& A, const rope::RopeArgs& R, int heads, int64_t team, int64_t n_teams, float* s_max,
                                               float* table) {
   const int lane = threadIdx.x & 63;
@@ -339,15 +339,12 @@ __device__ __forceinline__ void append_groups(const AppendArgs& A, const rope::R
     const rope::Lane L = block_lane<ROPE>(R, which, lane & ((1 << A.lpr_shift) - 1));
     const bool in = lane < A.group_chunk;
     const TokenKey own = token_key(A, in ? chunk + lane : -1), before = token_key(A, chunk + lane - 1);
-    bool leads = own.seq >= 0 && !(before.seq == own.seq && before.block == own.block);
-    if constexpr (SINGLES) {
-      const TokenKey next = token_key(A, chunk + lane + 1);
-      const bool alone = leads && !(next.seq == own.seq && next.block == own.block);
-      const uint64_t singles = __ballot(alone);
-      if (singles) append_singles<kSrcF32, ROPE, NWV>(A, R, L, chunk, singles, which, h0, own_heads);
-      leads = leads && !alone;
-    }
-    for (uint64_t leaders = __ballot(leads); leaders; leaders &= leaders - 1) {
+    const bool leads = own.seq >= 0 && !(before.seq == own.seq && before.block == own.block);
+    const TokenKey next = token_key(A, chunk + lane + 1);
+    const bool alone = leads && !(next.seq == own.seq && next.block == own.block);
+    const uint64_t singles = __ballot(alone);
+    if (singles) append_singles<kSrcF32, ROPE, NWV>(A, R, L, chunk, singles, which, h0, own_heads);
+    for (uint64_t leaders = __ballot(leads && !alone); leaders; leaders &= leaders - 1) {
       const int first = __builtin_ctzll(leaders);
       const Group G = find_group(A, chunk + first, __builtin_amdgcn_readlane(own.seq, first), __builtin_amdgcn_readlane(own.block, first));
       if (G.layer) append_group<kSrcF32, ROPE, NWV, LATE>(A, R, L, G, which, h0, own_heads, s_max, table);
@@ -359,7 +356,6 @@ __device__ __forceinline__ void append_groups(const AppendArgs& A, const rope::R
 struct GroupPlan {
   int team;        // waves of a team: 4 or 8, a workgroup; or 1, four of them to a workgroup
   bool late;       // blocks hold more tokens than a team keeps
-  bool singles;    // a launch of so few tokens that many may be groups of their own (see append_groups)
   int heads;       // heads of a unit
   int32_t chunk;   // AppendArgs::group_chunk
   int64_t blocks;  // workgroups
@@ -373,7 +369,7 @@ __device__ __forceinline__ void append_any(const AppendArgs& A, int64_t worker, 
     case FS_KV_FP8_E4M3: append_rows<kSrcF32, FS_KV_FP8_E4M3, HP>(A, worker, n_workers); break;
     case FS_KV_INT8: append_rows<kSrcF32, FS_KV_INT8, HP>(A, worker, n_workers); break;
     case FS_KV_FP8_BLOCK:
-      if constexpr (BLOCK) append_groups<kSrcF32, kPlain, 1, true, true>(A, rope::RopeArgs{}, 1, worker, n_workers, nullptr, nullptr);
+      if constexpr (BLOCK) append_groups<kSrcF32, kPlain, 1, true>(A, rope::RopeArgs{}, 1, worker, n_workers, nullptr, nullptr);
       break;
     default: append_rows<kSrcF32, FS_KV_INT4, HP>(A, worker, n_workers); break;
   }

@@ -590,6 +590,9 @@ template <int HD>
 __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_direct_kernel(DirectArgs D, uint32_t* status) {
   direct_item_of_grid<HD, false>(D, status);
 }
+// FP8_BLOCK: bound as FP8 with static scales is, whose rows it reads; the scales are half a line per block and eight heads.  (us, static /
+// per block: 64 sequences of 512 - 4096 tokens, 8 heads of 128, 55.9 / 56.8; 256 of 1024 - 8192 407 / 409; 128 of 1000 - 6000 at head_dim 64 80.7 /
+// 81.0 -- 94.7 while K's scale was loaded apart and went into the conversion.)
 template <int HD>
 __global__ __launch_bounds__(kThreads, mfma_wgs_per_cu(HD)) void mfma_block_direct_kernel(DirectArgs D, uint32_t* status) {
   direct_item_of_grid<HD, true>(D, status);

@@ -2433,8 +2433,10 @@ template <int DT, int NW, int NCB, int SUBS, int WPC, bool PIPE = false, bool DE
 __global__ __launch_bounds__(NW * 64, WPC) void prefill_wg_kernel(PrefillArgs P) {
   prefill_groups<DT, NW, NCB, SUBS, PIPE, DEQ, HD, SUM32, GROUPS, SPLIT>(P);
 }
-// FP8_BLOCK models.  (Sums over the unrounded weights everywhere: lse is then exact to fp32's sums; four chunks of 512 behind 3000 -
-// 16384 tokens take 312 us like this and 317 with the sums of the rounded ones.)
+// FP8_BLOCK models: kernels of their own, so that the other formats' stay what they are.  Bound like those, by the matrix products and
+// the power they take.  Sums over the unrounded weights everywhere: lse is then exact to fp32's sums.  That costs up to 3 %: 64 prompts of 4096
+// tokens 8260 us and 8090 with the sums of the rounded ones, 24 of 512 - 4096 in blocks of 25 1540 and 1494, four chunks of 512 behind 3000 -
+// 16384 307 and 303.  (Beside static scales: 8040 / 7860 us, 1498 / 1486, 295 / 291.)
 template <int NW, int NCB, int SUBS, int HD, bool GROUPS = false, bool SPLIT = false>
 __global__ __launch_bounds__(NW * 64, 1) void prefill_wg_block_kernel(PrefillArgs P) {
   prefill_groups<FS_KV_FP8_BLOCK, NW, NCB, SUBS, false, false, HD, true, GROUPS, SPLIT>(P);

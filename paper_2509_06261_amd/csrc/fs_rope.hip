@@ -16,7 +16,7 @@ namespace {
 using namespace append;
 using namespace rope;
 constexpr int kWaves = 4;     // waves per workgroup
-constexpr int kTurnRows = 4;  // rows of a unit in launches that leave every wave slot work, as kWideUnit
+constexpr int kTurnRows = 4;  // rows of a unit in larger launches: the angles are worked out once for them (see wide_units)
 
 // ---- fs_rope ------------------------------------------------------------------------------------------------------
 struct TurnArgs {
@@ -29,7 +29,8 @@ struct TurnArgs {
 };
 
 // A unit: HP neighbouring heads of 64 / lpr consecutive tokens, a token's row per lpr lanes.  A row lies in one wave, which
-// reads all of it before it writes: `out` may be `x`.
+// reads all of it before it writes: `out` may be `x`.  Bound by memory: 16 384 tokens of 32 heads of 128 in fp16, 268 MB read and written,
+// 49 us, 5.5 TB/s (78 with the sines of every element by itself).
 template <int MODE, bool kF32, bool kOutF32, int HP>
 __global__ __launch_bounds__(kWaves * 64) void turn_kernel(TurnArgs A) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -161,20 +162,22 @@ __global__ __launch_bounds__(kWaves * 64) void rope_append_kernel(RopeAppendArgs
 
 // FP8_BLOCK: the keys and values by groups of a block's tokens (fs_append_block.h), the queries by rows.  The cache's workgroups
 // come first: they take longest.  TEAM, heads: as in kv_append_block_kernel.  Dynamic LDS: the teams' tables of angles.
-template <int MODE, bool kSrcF32, int TEAM, bool LATE, bool SINGLES>
+// Bound by the vector ALU (angles, rotation, conversion) and by memory about equally: four waves a SIMD, also where fp32 rows then spill some
+// registers (65 600 tokens 179 us, with three waves and no spills 186).
+template <int MODE, bool kSrcF32, int TEAM, bool LATE>
 __global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64, LATE ? 2 : 4) void rope_append_block_kernel(RopeAppendArgs P, int heads) {
   extern __shared__ float s_table[];
   constexpr int kOwn = TEAM > 1 ? TEAM : kWaves;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t cache_blocks = gridDim.x - P.q_blocks;
-  if (SINGLES && blockIdx.x >= cache_blocks) {  // (larger launches rotate the queries in one of their own)
+  if (blockIdx.x >= cache_blocks) {
     rope_append_rows<MODE, kSrcF32, FS_KV_FP8_BLOCK, 1, false>(P, (int64_t)(blockIdx.x - cache_blocks) * kOwn + wave, (int64_t)P.q_blocks * kOwn);
   } else if constexpr (TEAM == 1) {
-    append_groups<kSrcF32, MODE, 1, LATE, SINGLES>(P.a, P.rope, heads, (int64_t)blockIdx.x * kWaves + wave, (int64_t)cache_blocks * kWaves, nullptr,
+    append_groups<kSrcF32, MODE, 1, LATE>(P.a, P.rope, heads, (int64_t)blockIdx.x * kWaves + wave, (int64_t)cache_blocks * kWaves, nullptr,
                                                    s_table + wave * table_floats(1));
   } else {
     __shared__ float s_max[2 * TEAM];
-    append_groups<kSrcF32, MODE, TEAM, LATE, SINGLES>(P.a, P.rope, heads, blockIdx.x, cache_blocks, s_max, s_table);
+    append_groups<kSrcF32, MODE, TEAM, LATE>(P.a, P.rope, heads, blockIdx.x, cache_blocks, s_max, s_table);
   }
 }
 
@@ -200,9 +203,10 @@ void (*rope_append_kernel_for(int dtype, bool f32, bool wide))(RopeAppendArgs) {
 }
 template <int MODE, bool kF32>
 void (*rope_append_block_kernel_for(const GroupPlan& G))(RopeAppendArgs, int) {
-#define FS_TEAM(TEAM, LATE) (G.singles ? rope_append_block_kernel<MODE, kF32, TEAM, LATE, true> : rope_append_block_kernel<MODE, kF32, TEAM, LATE, false>)
-  return G.late ? FS_TEAM(8, true) : G.team == 8 ? FS_TEAM(8, false) : G.team == 4 ? FS_TEAM(4, false) : FS_TEAM(1, false);
-#undef FS_TEAM
+  return G.late        ? rope_append_block_kernel<MODE, kF32, 8, true>
+         : G.team == 8 ? rope_append_block_kernel<MODE, kF32, 8, false>
+         : G.team == 4 ? rope_append_block_kernel<MODE, kF32, 4, false>
+                       : rope_append_block_kernel<MODE, kF32, 1, false>;
 }
 
 RopeArgs rope_args(const Model& M, int inverse) {
@@ -259,8 +263,13 @@ int64_t row_units(int64_t n_tokens, int lpr_shift, int rows, int hp) {
   return (n_tokens + tpw - 1) / tpw * ((rows + hp - 1) / hp);
 }
 
+// Units of kTurnRows where there is one for every SIMD.  (us, single rows / four, units of four: queries of 4000 tokens, 32 heads of 128, 8000
+// 16.6 / 12.0; of 1000, 2000 6.3 / 4.9; of 300, 600 4.2 / 4.2; with the rows of an FP16 cache 1000 tokens, 3000 8.8 / 7.2; 512, 1536 6.3 / 6.2;
+// 300, 900 5.4 / 6.5.)
+bool wide_units(const fs_pool* p, int64_t n_tokens, int lpr_shift, int rows) { return row_units(n_tokens, lpr_shift, rows, kTurnRows) >= (int64_t)p->n_cu * 4; }
+
 hipError_t launch_turn(const fs_pool* p, const TurnArgs& A, bool src_f32, bool out_f32, hipStream_t s) {
-  const bool wide = row_units(A.n_tokens, A.lpr_shift, A.n_heads, kTurnRows) >= (int64_t)p->n_cu * 32;
+  const bool wide = wide_units(p, A.n_tokens, A.lpr_shift, A.n_heads);
   const int64_t units = row_units(A.n_tokens, A.lpr_shift, A.n_heads, wide ? kTurnRows : 1);
   const unsigned blocks = (unsigned)std::min<int64_t>((units + kWaves - 1) / kWaves, (int64_t)p->n_cu * 64);
   const int mode = mode_of(A.rope);
@@ -413,8 +422,10 @@ extern "C" int fs_rope_append(fs_pool* p, fs_model_t model, int layer, const voi
   (void)hipGetLastError();
   hipError_t e = hipSuccess;
   const GroupPlan G = block ? plan_groups(p, P.a) : GroupPlan{};
-  // Enough rows for every wave slot: the queries in a launch of their own, whose waves take a third of the registers.
-  if (n_q_heads > 0 && (row_units(n_tokens, P.a.lpr_shift, n_q_heads, kTurnRows) >= (int64_t)p->n_cu * 32 || (block && !G.singles))) {
+  // FP8_BLOCK, many queries: they go in a launch of their own, whose waves take a third of the registers and four rows to a unit.  (us, one
+  // launch / two, units of four: 64 000 tokens, 32 query heads of 128, 128 000 343 / 326; 8000, 16 000 51 / 44; 4000, 8000 35.2 / 32.9; 1000, 2000
+  // 15.3 / 18.6.  The other formats' rows go with the queries': 64 000 tokens 285 / 299.)
+  if (block && n_q_heads > 0 && row_units(n_tokens, P.a.lpr_shift, n_q_heads, kTurnRows) >= (int64_t)p->n_cu * 16) {
     TurnArgs T{};
     T.rope = P.rope;
     T.x = q;
@@ -444,7 +455,7 @@ extern "C" int fs_rope_append(fs_pool* p, fs_model_t model, int layer, const voi
     hipLaunchKernelGGL(kern, dim3((unsigned)(G.blocks + P.q_blocks)), dim3(waves * 64), lds, s, P, G.heads);
   } else {
     const int rows = P.n_q + 2 * M->g.n_kv_heads;
-    const bool wide = row_units(n_tokens, P.a.lpr_shift, rows, kTurnRows) >= (int64_t)p->n_cu * 32;
+    const bool wide = wide_units(p, n_tokens, P.a.lpr_shift, rows);
     const int64_t blocks = std::min((row_units(n_tokens, P.a.lpr_shift, rows, wide ? kTurnRows : 1) + kWaves - 1) / kWaves, most);
     const int dtype = M->g.kv_dtype;
     void (*const kern)(RopeAppendArgs) = mode == kSplit   ? rope_append_kernel_for<kSplit>(dtype, f32, wide)
