@@ -372,10 +372,11 @@ def fs_rope_frequencies(rope: fs_rope_t) -> np.ndarray:
 
 
 def _token_stride(x):
-    """Elements from one token's [heads][head_dim] rows to the next one's; a token's rows themselves are contiguous."""
+    """Elements from one token's [heads][head_dim] rows to the next one's (of one token its own, so that a row shorter than the model's is
+    refused); a token's rows themselves are contiguous."""
     n, heads, d = x.shape
     assert x.stride(2) == 1 and (heads <= 1 or x.stride(1) == d)
-    return x.stride(0) if n > 1 else 0
+    return x.stride(0) if n > 1 else heads * d
 
 
 def fs_rope(pool, model, x, pos, out, inverse=False, stream=None):

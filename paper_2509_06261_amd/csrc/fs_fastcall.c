@@ -136,7 +136,7 @@ static int workspace(PyObject* o, void** out, uint64_t* bytes) {
   return 1;
 }
 
-/* rows [tokens][heads][head_dim] of fp16 or fp32, a token's rows contiguous; stride: elements from token to token (0: one token) */
+/* rows [tokens][heads][head_dim] of fp16 or fp32, a token's rows contiguous; stride: elements from token to token (one token: its own) */
 typedef struct {
   int64_t n, heads, d, stride;
   void* at;
@@ -170,7 +170,7 @@ static int rows_of(PyObject* o, rows_t* r) {
   r->n = v[0];
   r->heads = v[1];
   r->d = v[2];
-  r->stride = v[0] > 1 ? v[3] : 0;
+  r->stride = v[0] > 1 ? v[3] : v[1] * v[2];  /* (so that a row shorter than the model's is refused also here) */
   return address(o, &r->at);
 }
 static int same_shape(const rows_t* a, const rows_t* b) { return a->n == b->n && a->heads == b->heads && a->d == b->d; }

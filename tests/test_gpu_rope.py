@@ -313,3 +313,21 @@ def test_rotation_of_many_rows():
             some = np.concatenate([some[some != 77], [0, 1, 8999, 9000]])
             check_rotated(out[some].double().cpu().numpy(), x[some].double().cpu().numpy(), pos.cpu().numpy()[some], plain.frequencies(r, 10000.0, "none"), halves, "fp16" if dt == torch.float16 else "fp32")
         fs.fs_pool_destroy(pool)
+
+
+def test_rows_of_another_model_are_refused():
+    """Also of one token, whose stride nobody needs."""
+    import torch
+    c = Cache("fp16", 2, 64, 16, 1, np.array([5]), 3, fs.make_rope(64, 10000.0))
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for stream in (None, torch.cuda.current_stream().cuda_stream):  # natively and through ctypes
+        def rows(h, d, n=1):
+            return torch.ones((n, h, d), device="cuda", dtype=torch.float16)
+        fs.fs_rope(c.pool, c.model, rows(3, 64), one, rows(3, 64), stream=stream)
+        with pytest.raises(fs.FsError):
+            fs.fs_rope(c.pool, c.model, rows(3, 32), one, rows(3, 32), stream=stream)
+        fs.fs_rope_append(c.pool, c.model, 0, rows(4, 64), rows(2, 64), rows(2, 64), one, one, c.table, rows(4, 64), stream=stream)
+        for q, kv in (((4, 32), (2, 64)), ((4, 64), (1, 64)), ((4, 64), (2, 32))):
+            with pytest.raises(fs.FsError):
+                fs.fs_rope_append(c.pool, c.model, 0, rows(*q), rows(*kv), rows(*kv), one, one, c.table, rows(*q), stream=stream)
+    c.close()

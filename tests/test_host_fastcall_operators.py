@@ -57,7 +57,7 @@ def test_rope(got, dt):
         src = fs.FS_SRC_FP32 if dt == torch.float32 else fs.FS_SRC_FP16
         assert got["rope"] == [0x123, 2, x.data_ptr(), step, 6, src, pos.data_ptr(), 5, int(inverse), out.data_ptr(), 96, STREAM + 3]
     one = x[:1]
-    assert _fsfast.rope(vp(1), 2, one, ints(1), one, False, None) == 7 and got["rope"][3] == 0
+    assert _fsfast.rope(vp(1), 2, one, ints(1), one, False, None) == 7 and got["rope"][3] == 96
 
 
 @pytest.mark.parametrize("queries", [True, False])
