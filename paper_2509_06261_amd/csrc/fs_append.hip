@@ -22,13 +22,13 @@ __global__ __launch_bounds__(kWaves * 64) void kv_append_kernel(AppendArgs A) {
 }
 
 // FP8_BLOCK models.  TEAM: waves that work on a group together.
-template <bool kSrcF32, int TEAM, bool LATE>
+template <bool kSrcF32, int TEAM, bool LATE, bool AHEAD>
 __global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64) void kv_append_block_kernel(AppendArgs A, int heads) {
   if constexpr (TEAM == 1) {
-    append_groups<kSrcF32, kPlain, 1, LATE>(A, rope::RopeArgs{}, heads, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves, nullptr, nullptr);
+    append_groups<kSrcF32, kPlain, 1, LATE, AHEAD>(A, rope::RopeArgs{}, heads, (int64_t)blockIdx.x * kWaves + wave_id(), (int64_t)gridDim.x * kWaves, nullptr, nullptr);
   } else {
     __shared__ float s_max[2 * TEAM];
-    append_groups<kSrcF32, kPlain, TEAM, LATE>(A, rope::RopeArgs{}, heads, blockIdx.x, gridDim.x, s_max, nullptr);
+    append_groups<kSrcF32, kPlain, TEAM, LATE, AHEAD>(A, rope::RopeArgs{}, heads, blockIdx.x, gridDim.x, s_max, nullptr);
   }
 }
 
@@ -102,7 +102,8 @@ append::GroupPlan plan_groups(const fs_pool* p, const append::AppendArgs& A) {
   G.late = A.g.T > 8 * held;
   // Several heads to a unit, which share the group's angles and the search for it, where whole blocks of tokens make enough units.
   // (us, at most 2 / 4 / 8 heads: 65 600 tokens' keys and values, 8 heads of 128, blocks of 63: 154 / 136 / 141, without a rotation
-  // 82 / 80 / 89; blocks of 128: 219 / 171 / 155 and 123 / 107 / 102; of 16: 149 / 145 / 156; fp32: 196 / 179 / 207.)
+  // 82 / 80 / 89; blocks of 128: 219 / 171 / 155 and 123 / 107 / 102; of 16: 149 / 145 / 156; fp32: 196 / 179 / 207 -- all before a head's rows were
+  // requested ahead of the last one's work, which took 10 % off.)
   const int64_t groups = std::max<int64_t>(A.n_tokens / A.g.T, 1), full = (int64_t)p->n_cu * 8 / G.team;
   G.heads = (int)std::min<int64_t>(std::min(H, kUnitHeads), std::max<int64_t>(groups * 2 * H / full, 1));
   const int parts = 2 * ((H + G.heads - 1) / G.heads);
@@ -161,8 +162,10 @@ extern "C" int fs_kv_append(fs_pool* p, fs_model_t model, int layer, const void*
     const append::GroupPlan G = plan_groups(p, A);
     A.group_chunk = G.chunk;
     void (*kern)(AppendArgs, int) = nullptr;
-#define FS_APPEND(TEAM, LATE) (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE> : kv_append_block_kernel<false, TEAM, LATE>)
-    kern = G.late ? FS_APPEND(8, true) : G.team == 8 ? FS_APPEND(8, false) : G.team == 4 ? FS_APPEND(4, false) : FS_APPEND(1, false);
+#define FS_APPEND(TEAM, LATE, AHEAD) (A.src_f32 ? kv_append_block_kernel<true, TEAM, LATE, AHEAD> : kv_append_block_kernel<false, TEAM, LATE, AHEAD>)
+#define FS_HEADS(TEAM) (G.heads > 1 ? FS_APPEND(TEAM, false, true) : FS_APPEND(TEAM, false, false))
+    kern = G.late ? FS_APPEND(8, true, false) : G.team == 8 ? FS_HEADS(8) : G.team == 4 ? FS_HEADS(4) : FS_HEADS(1);
+#undef FS_HEADS
 #undef FS_APPEND
     (void)hipGetLastError();
     hipLaunchKernelGGL(kern, dim3((unsigned)G.blocks), dim3((G.team > 1 ? G.team : kWaves) * 64), 0, (hipStream_t)stream, A, G.heads);

@@ -153,13 +153,13 @@ __device__ __forceinline__ void load_block_row(const void* src, int64_t row, con
 
 // A group's rows of `heads` neighbouring heads from h0 on, K or V, by a team of NWV waves (a workgroup; or one wave, NWV = 1): its
 // tokens over the team's lanes, lpr lanes to a row, kSteps rows to a lane.  Those stay in registers between the maximum and the
-// conversion; the next head's rows are requested before the waves meet for the maximum.  LATE: a group of more rows than that reads
-// the rest twice.  The angles of the tokens that are kept are worked out once for all heads, in LDS.
+// conversion; the next head's rows are requested before the waves meet for the maximum, or (AHEAD) before this head's are widened, which
+// takes registers of their own.  LATE: a group of more rows than that reads the rest twice.  The angles of the tokens that are kept are worked out once for all heads, in LDS.
 // s_max: LDS, 2 * NWV floats; table: LDS, table_floats<NWV>() floats.
 constexpr int kSteps = 4;
 // A lane's eight elements are four pairs; two numbers each.
 constexpr int table_floats(int team) { return team * 64 * kSteps * kEpl; }
-template <bool kSrcF32, int ROPE, int NWV, bool LATE>
+template <bool kSrcF32, int ROPE, int NWV, bool LATE, bool AHEAD>
 __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::RopeArgs& R, const rope::Lane& L, const Group& G, int which, int h0,
                                              int heads, float* s_max, float* table) {
   const int lane = threadIdx.x & 63;
@@ -172,19 +172,19 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
   const int64_t t0 = wave * tpw + (lane >> A.lpr_shift);
   const int step = NWV * tpw;
   int slot[kSteps];
-  rope::Raw<kSrcF32> own[kSteps];
+  rope::Raw<kSrcF32> own[kSteps], ahead[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const int64_t t = t0 + (int64_t)s * step;
     slot[s] = t < G.n ? A.pos[G.first + t] - G.block * g.T : -1;
   }
-  auto request = [&](int head) {
+  auto request = [&](int head, rope::Raw<kSrcF32> (&to)[kSteps]) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
       if (slot[s] >= 0)
-        load_block_row<kSrcF32, ROPE>(src, (G.first + t0 + (int64_t)s * step) * stride + (int64_t)head * g.D, L, which, own[s]);
+        load_block_row<kSrcF32, ROPE>(src, (G.first + t0 + (int64_t)s * step) * stride + (int64_t)head * g.D, L, which, to[s]);
   };
-  request(h0);
+  request(h0, own);
   int in_table = 0;  // tokens: all that are kept in registers
   if constexpr (ROPE != kPlain) {
     if (turned) {
@@ -221,6 +221,10 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (AHEAD) {
+      if (k + 1 < heads) request(head + 1, ahead);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     float x[kSteps][kEpl];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -237,7 +241,7 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
       }
       amax = amax8(amax, x[s]);
     }
-    if (k + 1 < heads) request(head + 1);
+    if (!AHEAD && k + 1 < heads) request(head + 1, own);
     amax = wave_max(amax);
     if constexpr (NWV > 1) {
       float* const m = s_max + (k & 1) * NWV;  // (two of them, in turn: a wave is at most one barrier ahead)
@@ -260,6 +264,10 @@ __device__ __forceinline__ void append_group(const AppendArgs& A, const rope::Ro
         late_row(head, t, y);
         put_codes(A, B.rows, A.pos[G.first + t] - G.block * g.T, L, split, y, f);
       }
+    }
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) own[s] = ahead[s];
     }
   }
   if constexpr (NWV > 1) __syncthreads();  // (the next group's maxima and table)
@@ -324,7 +332,7 @@ __device__ __forceinline__ void append_singles(const AppendArgs& A, const rope::
 // One append, dealt to n_teams teams of NWV waves; this one is number `team`.  A unit: the groups that begin among
 // A.group_chunk neighbouring tokens, of them `heads` heads' K or V rows.  Groups of one token, a decode step's, are worked on side by side
 // (16 384 of them 55 us; as groups like the others, one after the other, 385; prompts take the same with either, 125 and 123).
-template <bool kSrcF32, int ROPE, int NWV, bool LATE>
+template <bool kSrcF32, int ROPE, int NWV, bool LATE, bool AHEAD>
 __device__ __forceinline__ void append_groups(const AppendArgs& A, const rope::RopeArgs& R, int heads, int64_t team, int64_t n_teams, float* s_max,
                                               float* table) {
   const int lane = threadIdx.x & 63;
@@ -347,7 +355,7 @@ __device__ __forceinline__ void append_groups(const AppendArgs& A, const rope::R
     for (uint64_t leaders = __ballot(leads && !alone); leaders; leaders &= leaders - 1) {
       const int first = __builtin_ctzll(leaders);
       const Group G = find_group(A, chunk + first, __builtin_amdgcn_readlane(own.seq, first), __builtin_amdgcn_readlane(own.block, first));
-      if (G.layer) append_group<kSrcF32, ROPE, NWV, LATE>(A, R, L, G, which, h0, own_heads, s_max, table);
+      if (G.layer) append_group<kSrcF32, ROPE, NWV, LATE, AHEAD>(A, R, L, G, which, h0, own_heads, s_max, table);
     }
   }
 }
@@ -369,7 +377,7 @@ __device__ __forceinline__ void append_any(const AppendArgs& A, int64_t worker, 
     case FS_KV_FP8_E4M3: append_rows<kSrcF32, FS_KV_FP8_E4M3, HP>(A, worker, n_workers); break;
     case FS_KV_INT8: append_rows<kSrcF32, FS_KV_INT8, HP>(A, worker, n_workers); break;
     case FS_KV_FP8_BLOCK:
-      if constexpr (BLOCK) append_groups<kSrcF32, kPlain, 1, true>(A, rope::RopeArgs{}, 1, worker, n_workers, nullptr, nullptr);
+      if constexpr (BLOCK) append_groups<kSrcF32, kPlain, 1, true, false>(A, rope::RopeArgs{}, 1, worker, n_workers, nullptr, nullptr);
       break;
     default: append_rows<kSrcF32, FS_KV_INT4, HP>(A, worker, n_workers); break;
   }

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kWaves * 64) void rope_append_kernel(RopeAppendArgs
 // come first: they take longest.  TEAM, heads: as in kv_append_block_kernel.  Dynamic LDS: the teams' tables of angles.
 // Bound by the vector ALU (angles, rotation, conversion) and by memory about equally: four waves a SIMD, also where fp32 rows then spill some
 // registers (65 600 tokens 179 us, with three waves and no spills 186).
-template <int MODE, bool kSrcF32, int TEAM, bool LATE>
+template <int MODE, bool kSrcF32, int TEAM, bool LATE, bool AHEAD>
 __global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64, LATE ? 2 : 4) void rope_append_block_kernel(RopeAppendArgs P, int heads) {
   extern __shared__ float s_table[];
   constexpr int kOwn = TEAM > 1 ? TEAM : kWaves;
@@ -173,11 +173,11 @@ __global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64, LATE ? 2 : 4) void
   if (blockIdx.x >= cache_blocks) {
     rope_append_rows<MODE, kSrcF32, FS_KV_FP8_BLOCK, 1, false>(P, (int64_t)(blockIdx.x - cache_blocks) * kOwn + wave, (int64_t)P.q_blocks * kOwn);
   } else if constexpr (TEAM == 1) {
-    append_groups<kSrcF32, MODE, 1, LATE>(P.a, P.rope, heads, (int64_t)blockIdx.x * kWaves + wave, (int64_t)cache_blocks * kWaves, nullptr,
+    append_groups<kSrcF32, MODE, 1, LATE, AHEAD>(P.a, P.rope, heads, (int64_t)blockIdx.x * kWaves + wave, (int64_t)cache_blocks * kWaves, nullptr,
                                                    s_table + wave * table_floats(1));
   } else {
     __shared__ float s_max[2 * TEAM];
-    append_groups<kSrcF32, MODE, TEAM, LATE>(P.a, P.rope, heads, blockIdx.x, cache_blocks, s_max, s_table);
+    append_groups<kSrcF32, MODE, TEAM, LATE, AHEAD>(P.a, P.rope, heads, blockIdx.x, cache_blocks, s_max, s_table);
   }
 }
 
@@ -203,10 +203,13 @@ void (*rope_append_kernel_for(int dtype, bool f32, bool wide))(RopeAppendArgs) {
 }
 template <int MODE, bool kF32>
 void (*rope_append_block_kernel_for(const GroupPlan& G))(RopeAppendArgs, int) {
-  return G.late        ? rope_append_block_kernel<MODE, kF32, 8, true>
-         : G.team == 8 ? rope_append_block_kernel<MODE, kF32, 8, false>
-         : G.team == 4 ? rope_append_block_kernel<MODE, kF32, 4, false>
-                       : rope_append_block_kernel<MODE, kF32, 1, false>;
+  // Rows ahead where a unit has several heads and the registers suffice.  (65 600 tokens' keys and values, 8 heads of 128, us without / with them:
+  // fp16 in blocks of 63 137 / 125, of 128 174 / 166, of 16 148 / 138, and without a rotation 81 / 73, 108 / 95, 90 / 83; fp32 141 / 133 without a
+  // rotation, but 198 / 261 with one.  With one head to a unit the kernel is the slower for them: a prompt of 777 tokens 12.5 / 14.)
+  constexpr bool kAhead = !kF32 && MODE != kMixed;
+#define FS_HEADS(TEAM) (kAhead && G.heads > 1 ? rope_append_block_kernel<MODE, kF32, TEAM, false, kAhead> : rope_append_block_kernel<MODE, kF32, TEAM, false, false>)
+  return G.late ? rope_append_block_kernel<MODE, kF32, 8, true, false> : G.team == 8 ? FS_HEADS(8) : G.team == 4 ? FS_HEADS(4) : FS_HEADS(1);
+#undef FS_HEADS
 }
 
 RopeArgs rope_args(const Model& M, int inverse) {
