@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kWaves * 64) void rope_append_kernel(RopeAppendArgs
 // FP8_BLOCK: the keys and values by groups of a block's tokens (fs_append_block.h), the queries by rows.  The cache's workgroups
 // come first: they take longest.  TEAM, heads: as in kv_append_block_kernel.  Dynamic LDS: the teams' tables of angles.
 // Bound by the vector ALU (angles, rotation, conversion) and by memory about equally: four waves a SIMD, also where fp32 rows then spill some
-// registers (65 600 tokens 179 us, with three waves and no spills 186).
+// registers (65 600 tokens' keys and values, when this was chosen, 179 us and with three waves 186; with tokens of a group each beside them 198).
 template <int MODE, bool kSrcF32, int TEAM, bool LATE, bool AHEAD>
 __global__ __launch_bounds__((TEAM > 1 ? TEAM : kWaves) * 64, LATE ? 2 : 4) void rope_append_block_kernel(RopeAppendArgs P, int heads) {
   extern __shared__ float s_table[];
